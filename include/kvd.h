@@ -387,6 +387,80 @@ kvd_status kvd_decode_attention_rows(kvd_ctx *ctx, int layer, int n_rows, const 
 kvd_status kvd_prefill_attention(kvd_ctx *ctx, int layer, int n_rows, const void *q, const int32_t *q_pos,
                                  const kvd_kv_segment *segs, int n_segs, float scale, void *out, void *stream);
 
+/* kvd_decode_attention behind a prefix that ALL sequences of the batch share (one system prompt, one document): `prefix`
+ * (HOST, one segment) is attended by every sequence in addition to its own segs[b][*], as if it were listed among them --
+ * same visibility rule, same definition -- but its keys and values are read from memory once for the batch instead of once
+ * per sequence: the queries of all sequences are the rows of tensor-core tiles over the prefix, and the partials join each
+ * sequence's own in the merge.  prefix->len == 0 is kvd_decode_attention.  The split of the prefix depends on the batch and
+ * its weights are rounded to the element type before the second product, so the bits are not those of kvd_decode_attention
+ * (same tolerance against the definition), and a sequence's bits may depend on the batch's size.  The prefix must not
+ * overlap a sequence's own segments in position.  n_segs <= KVD_MAX_SEGMENTS.  Needs an attached workspace. */
+kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int batch, const void *q, const int32_t *q_pos,
+                                       const kvd_kv_segment *prefix, const kvd_kv_segment *segs, int n_segs, float scale,
+                                       void *out, void *stream);
+
+/* ---- A cache ranked by accumulated attention weight (the eviction policies that the paper's Section 5 compares the
+ * oldest-first window with keep the keys that have been attended most) ----
+ * What the key at position p has weighed so far is one fp32 number per token and layer, summed over all query heads and all
+ * queries that have attended it:  w_p = sum over queries t and heads h of softmax_j(scale q_th . k_j)[p].
+ *
+ * kvd_decode_attention_weights is kvd_decode_attention (same arguments, same output bits) that also adds what the call's one
+ * query per sequence gives every key:
+ *   weights_out[b * weights_stride + p] = weights_in[b * weights_stride + p] + sum_h p_h(p)     for 0 <= p < n_positions
+ * (DEVICE fp32, weights_in may be NULL for zeros, or the same array as weights_out; otherwise the two do not overlap).
+ * Positions the query does not see, or that no segment holds, keep their weight.  In a cache whose slots are not in
+ * the order of positions (kvd_cache_evict) a segment with first_pos = 0 and q_pos = len - 1 numbers the slots.
+ * KVD_ERR_CAPACITY when a visible key's position is >= n_positions (at most 2^30).  scratch: DEVICE, 256-byte aligned, at
+ * least kvd_weights_scratch_bytes(desc, batch, span) for the longest visible span of a sequence; the scores pass through it.
+ * A head whose row of scores is all minus infinity adds nothing; a NaN among a head's scores makes the weights of its keys
+ * NaN.  Heads are added in ascending order: equal calls give equal bits. */
+size_t kvd_weights_scratch_bytes(const kvd_model_desc *desc, int batch, int max_span);
+kvd_status kvd_decode_attention_weights(kvd_ctx *ctx, int layer, int batch, const void *q, const int32_t *q_pos,
+                                        const kvd_kv_segment *segs, int n_segs, float scale, void *out,
+                                        const float *weights_in, float *weights_out, int64_t weights_stride,
+                                        int n_positions, void *scratch, size_t scratch_bytes, void *stream);
+
+/* The same sums for many query tokens of one sequence at once (a prompt, or the last rows of one as an observation window):
+ *   weights_out[p] = weights_in[p] + sum over rows r and heads h of p_rh(p)     for 0 <= p < n_positions
+ * with q, q_pos (DEVICE), segs as in kvd_prefill_attention; values are not read and no output is computed (v of a segment
+ * may be NULL).  Two passes of scores on tcgen05.mma: every row's maximum and sum, then the columns' weights; partial sums
+ * are added in a fixed order.  scratch: DEVICE, 256-byte aligned, >= kvd_prefill_weights_scratch_bytes(desc, n_rows,
+ * n_positions).  KVD_ERR_CAPACITY when a segment reaches past n_positions (at most 2^30).  bf16 and fp16 contexts. */
+size_t kvd_prefill_weights_scratch_bytes(const kvd_model_desc *desc, int n_rows, int n_positions);
+kvd_status kvd_prefill_attention_weights(kvd_ctx *ctx, int layer, int n_rows, const void *q, const int32_t *q_pos,
+                                         const kvd_kv_segment *segs, int n_segs, float scale, const float *weights_in,
+                                         float *weights_out, int n_positions, void *scratch, size_t scratch_bytes,
+                                         void *stream);
+
+/* Caches of a batch, `slots` keys of room each (DEVICE; element (slot j, head h, channel c) of sequence b's keys at
+ * k[(b * slots + j) * row_stride + h * d_head + c], in the context's element type; positions and weights [batch][slots]). */
+typedef struct {
+  void *k;
+  void *v;
+  int32_t *positions; /* of the slots' tokens; in: NULL = slot j holds position j, out: NULL = not written */
+  float *weights;     /* out: NULL = not written */
+  int64_t row_stride; /* elements, a multiple of 16 bytes */
+  int64_t slots;
+} kvd_ranked_cache;
+#define KVD_MAX_EVICT_SLOTS 131072
+
+/* Evict from the caches of a batch until each holds `keep` keys.  Sequence b has lens[b] (HOST) keys in slots 0 ..
+ * lens[b]-1; min(keep, lens[b]) of them stay: first the protected ones (position < protect_below, the attention sinks, or
+ * position >= protect_from[b], the recent tokens; protect_from HOST, NULL = none), then the others; by weight among either,
+ * the lower slot first among equals.  A NaN counts as minus infinity, -0 as +0.
+ *   out         the kept keys in slots 0 .. min(keep, lens[b])-1: one whose slot is below that number keeps its slot, the
+ *               others fill the freed slots in ascending order, so an eviction in place (out's k, v, row_stride and slots
+ *               equal to in's) moves as few keys as possible.  Arrays of `out` that are not those of `in` must not overlap
+ *               them.  k and v NULL in both: only the lists, positions and weights are made.
+ *   slots_out   DEVICE int32 [batch][out->slots]: the slot each kept key came from.
+ *   evicted_out DEVICE int32 [batch][evicted_stride]: the positions of the evicted keys, by ascending slot (what
+ *               kvd_recompute_kv rebuilds from the residual store when they are needed after all); lens[b] - keep entries
+ *               are written, evicted_stride holds the most of them (KVD_ERR_CAPACITY).  NULL only when nothing is evicted.
+ * lens[b] <= KVD_MAX_EVICT_SLOTS.  Two launches; nothing is launched when any argument is rejected. */
+kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_cache *in, const int32_t *lens, int keep,
+                           int32_t protect_below, const int32_t *protect_from, const kvd_ranked_cache *out,
+                           int32_t *slots_out, int32_t *evicted_out, int64_t evicted_stride, void *stream);
+
 /* RECOMPUTE_KV and ATTENTION of Algorithm 1 in one pass for the evicted tokens (Eq. 13-14 feeding
  * Eq. 6-7): the keys and values rebuilt from the residual rows of ranges[b] are consumed inside the
  * recompute kernel -- the rotated key of a row is multiplied with the queries of its KV head, the value

@@ -45,6 +45,8 @@ EXPORTED_SYMBOLS = (
     "kvd_recompute_kv_step",
     "kvd_decode_attention", "kvd_decode_attention_rows", "kvd_prefill_attention", "kvd_decode_attention_static", "kvd_memory_stats", "kvd_poll_status", "kvd_selftest_wait_timeout", "kvd_build_has_checks", "kvd_selftest_bounds_check", "kvd_set_trace", "kvd_trace_bytes", "kvd_launch_count", "kvd_last_cuda_error",
     "kvd_status_string", "kvd_version",
+    "kvd_shared_prefix_attention", "kvd_weights_scratch_bytes", "kvd_decode_attention_weights", "kvd_prefill_weights_scratch_bytes",
+    "kvd_prefill_attention_weights", "kvd_cache_evict",
     # include/kvd_scaffold.h: the parts of a decoder layer around the hot path, for whole-stack tests and benchmarks
     "kvd_scaffold_linear_create", "kvd_scaffold_linear_destroy", "kvd_scaffold_linear_out_cols", "kvd_scaffold_linear",
     "kvd_scaffold_query_finish", "kvd_scaffold_add_rows", "kvd_scaffold_gated_act", "kvd_scaffold_embed",
@@ -90,6 +92,11 @@ class kvd_mem_stats(ctypes.Structure):
                 ("per_layer_residual_bytes_per_token", ctypes.c_uint64)]
 
 
+class kvd_ranked_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("row_stride", ctypes.c_int64), ("slots", ctypes.c_int64)]
+
+
 class KvdError(RuntimeError):
     def __init__(self, status: int, what: str, detail: str = ""):
         self.status = status
@@ -102,7 +109,8 @@ class KvdError(RuntimeError):
 _lib: Optional[ctypes.CDLL] = None
 _calls = None  # the C half of the binding: the calls of a decode step without ctypes (csrc/kvd_pycall.c)
 _CALLS = ("kvd_reset_sequence", "kvd_checkpoint_residual", "kvd_recompute_kv", "kvd_recompute_kv_step", "kvd_decode_step_kv",
-          "kvd_decode_attention", "kvd_prefill_attention")
+          "kvd_decode_attention", "kvd_prefill_attention", "kvd_shared_prefix_attention", "kvd_decode_attention_weights",
+          "kvd_prefill_attention_weights", "kvd_cache_evict")
 
 
 class _NoCalls:
@@ -183,6 +191,21 @@ def load() -> ctypes.CDLL:
     lib.kvd_decode_attention_rows.restype = i32
     lib.kvd_prefill_attention.argtypes = [vp, i32, i32, vp, vp, vp, i32, ctypes.c_float, vp, vp]
     lib.kvd_prefill_attention.restype = i32
+    lib.kvd_shared_prefix_attention.argtypes = [vp, i32, i32, vp, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(kvd_kv_segment), vp, i32,
+                                                ctypes.c_float, vp, vp]
+    lib.kvd_shared_prefix_attention.restype = i32
+    lib.kvd_weights_scratch_bytes.argtypes = [ctypes.POINTER(kvd_model_desc), i32, i32]
+    lib.kvd_weights_scratch_bytes.restype = sz
+    lib.kvd_decode_attention_weights.argtypes = [vp, i32, i32, vp, ctypes.POINTER(ctypes.c_int32), vp, i32, ctypes.c_float, vp, vp, vp, i64, i32,
+                                                 vp, sz, vp]
+    lib.kvd_decode_attention_weights.restype = i32
+    lib.kvd_prefill_weights_scratch_bytes.argtypes = [ctypes.POINTER(kvd_model_desc), i32, i32]
+    lib.kvd_prefill_weights_scratch_bytes.restype = sz
+    lib.kvd_prefill_attention_weights.argtypes = [vp, i32, i32, vp, vp, vp, i32, ctypes.c_float, vp, vp, i32, vp, sz, vp]
+    lib.kvd_prefill_attention_weights.restype = i32
+    lib.kvd_cache_evict.argtypes = [vp, i32, ctypes.POINTER(kvd_ranked_cache), ctypes.POINTER(ctypes.c_int32), i32, ctypes.c_int32,
+                                    ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(kvd_ranked_cache), vp, vp, i64, vp]
+    lib.kvd_cache_evict.restype = i32
     lib.kvd_set_dtype.argtypes = [vp, i32]
     lib.kvd_set_dtype.restype = i32
     lib.kvd_store_bytes_fp8.argtypes = [ctypes.POINTER(kvd_model_desc), i32]
@@ -304,6 +327,14 @@ def kvd_fp4_scratch_bytes(desc: kvd_model_desc, max_rows: int) -> int:
     return int(load().kvd_fp4_scratch_bytes(ctypes.byref(desc), max_rows))
 
 
+def kvd_weights_scratch_bytes(desc: kvd_model_desc, batch: int, max_span: int) -> int:
+    return int(load().kvd_weights_scratch_bytes(ctypes.byref(desc), batch, max_span))
+
+
+def kvd_prefill_weights_scratch_bytes(desc: kvd_model_desc, n_rows: int, n_positions: int) -> int:
+    return int(load().kvd_prefill_weights_scratch_bytes(ctypes.byref(desc), n_rows, n_positions))
+
+
 def kvd_workspace_bytes(desc: kvd_model_desc) -> int:
     return int(load().kvd_workspace_bytes(ctypes.byref(desc)))
 
@@ -376,6 +407,15 @@ def _marshal_segments(batch: int, q_pos, segs):
             e.v = v if isinstance(v, int) else _ptr(v)
             e.row_stride, e.first_pos, e.len = int(stride), int(first), int(ln)
     return n_segs, pos_arr, seg_arr
+
+
+# (k, v, positions, weights, row_stride, slots): the caches of a batch, see kvd_ranked_cache; tensors or None
+RankedCache = Tuple[object, object, object, object, int, int]
+
+
+def _marshal_cache(cache: RankedCache) -> kvd_ranked_cache:
+    k, v, positions, weights, row_stride, slots = cache
+    return kvd_ranked_cache(_ptr(k), _ptr(v), _ptr(positions), _ptr(weights), int(row_stride), int(slots))
 
 
 def _marshal_ranges(ranges, outputs: bool = True):
@@ -541,6 +581,63 @@ class Kvd:
             n_segs, _, seg_arr = _marshal_segments(1, [0], [list(segs)])
             st = self._lib.kvd_prefill_attention(self._h, layer, n_rows, _ptr(q), _ptr(q_pos_dev), seg_arr, n_segs, float(scale), _ptr(out), stream)
         self._check(st, "kvd_prefill_attention")
+
+    def kvd_shared_prefix_attention(self, layer: int, batch: int, q, q_pos: Sequence[int], prefix: Segment,
+                                    segs: Sequence[Sequence[Segment]], scale: float, out, stream=None) -> None:
+        """Decode attention of a batch behind one shared segment; segs: each sequence's own segments."""
+        stream = _stream(stream)
+        st = _calls.kvd_shared_prefix_attention(self._addr, layer, batch, q, q_pos, prefix, segs, scale, out, stream)
+        if st < 0:
+            n_segs, pos_arr, seg_arr = _marshal_segments(batch, q_pos, segs)
+            k, v, row_stride, first, ln = prefix
+            pre = kvd_kv_segment(k if isinstance(k, int) else _ptr(k), v if isinstance(v, int) else _ptr(v), int(row_stride), int(first), int(ln))
+            st = self._lib.kvd_shared_prefix_attention(self._h, layer, batch, _ptr(q), pos_arr, ctypes.byref(pre), seg_arr, n_segs, float(scale),
+                                                       _ptr(out), stream)
+        self._check(st, "kvd_shared_prefix_attention")
+
+    def kvd_decode_attention_weights(self, layer: int, batch: int, q, q_pos: Sequence[int], segs: Sequence[Sequence[Segment]], scale: float, out,
+                                     weights_in, weights_out, weights_stride: int, n_positions: int, scratch, stream=None) -> None:
+        """kvd_decode_attention that also adds every key's weight: weights_in (or None) + weights -> weights_out, float32
+        [batch, weights_stride]; scratch: a uint8 device tensor of kvd_weights_scratch_bytes."""
+        stream = _stream(stream)
+        size = scratch.numel() * scratch.element_size()
+        st = _calls.kvd_decode_attention_weights(self._addr, layer, batch, q, q_pos, segs, scale, out, weights_in, weights_out, weights_stride,
+                                                 n_positions, scratch, size, stream)
+        if st < 0:
+            n_segs, pos_arr, seg_arr = _marshal_segments(batch, q_pos, segs)
+            st = self._lib.kvd_decode_attention_weights(self._h, layer, batch, _ptr(q), pos_arr, seg_arr, n_segs, float(scale), _ptr(out),
+                                                        _ptr(weights_in), _ptr(weights_out), weights_stride, n_positions, _ptr(scratch), size, stream)
+        self._check(st, "kvd_decode_attention_weights")
+
+    def kvd_prefill_attention_weights(self, layer: int, n_rows: int, q, q_pos_dev, segs: Sequence[Segment], scale: float, weights_in, weights_out,
+                                      n_positions: int, scratch, stream=None) -> None:
+        """The keys' weights over many query rows of one sequence; q_pos_dev: int32 device tensor [n_rows], weights float32
+        [n_positions], scratch: a uint8 device tensor of kvd_prefill_weights_scratch_bytes."""
+        stream = _stream(stream)
+        size = scratch.numel() * scratch.element_size()
+        st = _calls.kvd_prefill_attention_weights(self._addr, layer, n_rows, q, q_pos_dev, segs, scale, weights_in, weights_out, n_positions, scratch,
+                                                  size, stream)
+        if st < 0:
+            n_segs, _, seg_arr = _marshal_segments(1, [0], [list(segs)])
+            st = self._lib.kvd_prefill_attention_weights(self._h, layer, n_rows, _ptr(q), _ptr(q_pos_dev), seg_arr, n_segs, float(scale),
+                                                         _ptr(weights_in), _ptr(weights_out), n_positions, _ptr(scratch), size, stream)
+        self._check(st, "kvd_prefill_attention_weights")
+
+    def kvd_cache_evict(self, batch: int, cache: RankedCache, lens: Sequence[int], keep: int, protect_below: int,
+                        protect_from: Optional[Sequence[int]], cache_out: RankedCache, slots_out, evicted_out, evicted_stride: int,
+                        stream=None) -> None:
+        """cache, cache_out: (k, v, positions, weights, row_stride, slots per sequence), the same tuple for an eviction in place."""
+        stream = _stream(stream)
+        st = _calls.kvd_cache_evict(self._addr, batch, cache, lens, keep, protect_below, protect_from, cache_out, slots_out, evicted_out,
+                                    evicted_stride, stream)
+        if st < 0:
+            n = max(batch, 1)
+            a, b = _marshal_cache(cache), _marshal_cache(cache_out)
+            len_arr = (ctypes.c_int32 * n)(*[int(x) for x in lens])
+            from_arr = None if protect_from is None else (ctypes.c_int32 * n)(*[int(x) for x in protect_from])
+            st = self._lib.kvd_cache_evict(self._h, batch, ctypes.byref(a), len_arr, keep, protect_below, from_arr, ctypes.byref(b), _ptr(slots_out),
+                                           _ptr(evicted_out), evicted_stride, stream)
+        self._check(st, "kvd_cache_evict")
 
     def kvd_decode_attention_recompute(self, layer: int, batch: int, q, q_pos: Sequence[int],
                                        ranges: Sequence[Tuple[int, int, int]], rows, positions, n_rows: int,

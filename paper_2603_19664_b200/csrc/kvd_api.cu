@@ -901,12 +901,12 @@ static kvd_status check_segments(const kvd_ctx *ctx, int batch, const int32_t *q
 }
 
 // Describe one launch over sequences b0 .. b0 + nb - 1 (nb <= AT_MAX_SEQS): segments, visible range, the
-// split into chunks and the slots of the partial arrays.  pre_parts[b] (may be NULL) slots are left
+// split into chunks and the slots of the partial arrays.  pre_parts[i] (may be NULL; of sequence b0 + i) slots are left
 // in front of a sequence's chunks for partials that another kernel writes (fused recompute); the
 // merge kernel combines them with the chunks, in slot order.
 static kvd_status build_attn_launch(kvd_ctx *ctx, const LayerState &ls, int b0, int nb, const void *q,
                                     const int32_t *q_pos, const kvd_kv_segment *segs, int n_segs, float scale,
-                                    void *out, const int *pre_parts, AttnLaunch &L) {
+                                    void *out, const int *pre_parts, AttnLaunch &L, bool tails = true) {
   const kvd_model_desc &d = ctx->desc;
   int parts = 0, slots = 0, streamed_slots = 0;
   L.tail = false;
@@ -940,7 +940,7 @@ static kvd_status build_attn_launch(kvd_ctx *ctx, const LayerState &ls, int b0, 
     S.lo_pos = lo;
     S.hi_pos = hi;
     S.part_base = parts;
-    const int pre = pre_parts ? pre_parts[b] : 0;
+    const int pre = pre_parts ? pre_parts[i] : 0;
     streamed_slots += pre;
     if (max_last < 0 || hi < lo) {
       S.n_chunks = 0;
@@ -957,7 +957,8 @@ static kvd_status build_attn_launch(kvd_ctx *ctx, const LayerState &ls, int b0, 
       // merge kernel takes them beside the partials it fetches (attn_tail).  FP8 step with a streaming launch for the one key /
       // without, us: Gemma-3-4B layer, 4096 rows 31.0 / 27.3, Qwen3-4B layer 4 x 2000 59 / 55.5.  (Every key there is a round
       // of shuffles in one warp.)  Each sequence by itself: what attends it does not depend on its neighbours.
-      if (pre_parts && hi - lo < AT_TAIL_KEYS) {
+      // (tails: the merge kernel has that form for the shape.)
+      if (pre_parts && tails && hi - lo < AT_TAIL_KEYS) {
         S.n_chunks = 0;
         L.tail = true;
       }
@@ -1012,6 +1013,158 @@ extern "C" kvd_status kvd_decode_attention(kvd_ctx *ctx, int layer, int batch, c
     st = launch_attention(ctx, L, d.d_head, group, stream);
     if (st != KVD_OK) return st;
   }
+  return KVD_OK;
+}
+
+extern "C" kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int batch, const void *q, const int32_t *q_pos,
+                                                  const kvd_kv_segment *prefix, const kvd_kv_segment *segs, int n_segs,
+                                                  float scale, void *out, void *stream_) {
+  if (!ctx || batch < 0 || n_segs < 0 || n_segs > KVD_MAX_SEGMENTS) return KVD_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= ctx->desc.n_layers) return KVD_ERR_INVALID_ARG;
+  const LayerState &ls = ctx->layers[layer];
+  if (!ls.set) return KVD_ERR_STATE;
+  if (!ctx->part_o) return KVD_ERR_STATE;
+  if (ctx->dtype == KVD_DTYPE_F32) return KVD_ERR_UNSUPPORTED;
+  if (batch == 0) return KVD_OK;
+  if (!q || !q_pos || !prefix || !out || (n_segs > 0 && !segs)) return KVD_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out)) return KVD_ERR_ALIGNMENT;
+  const kvd_model_desc &d = ctx->desc;
+  if (batch > d.max_batch) return KVD_ERR_CAPACITY;
+  const int group = d.n_q_heads / d.n_kv_heads;
+  kvd_status st = check_segments(ctx, batch, q_pos, segs, n_segs);
+  if (st == KVD_OK) st = check_segments(ctx, 1, q_pos, prefix, 1);
+  if (st != KVD_OK) return st;
+  if (prefix->len > 0) {
+    if (prefix->row_stride >= (int64_t{1} << 38)) return KVD_ERR_SHAPE;  // (a tensor map's strides are below 2^40 bytes)
+    for (int64_t i = 0; i < static_cast<int64_t>(batch) * n_segs; ++i) {
+      const int64_t a = segs[i].first_pos, p = prefix->first_pos;
+      if (segs[i].len > 0 && a < p + prefix->len && p < a + segs[i].len) return KVD_ERR_INVALID_ARG;
+    }
+  }
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  // live keys of a few positions are left to the merge kernel where it exists in that form (attn_launch_pair)
+  const bool tails = (d.d_head == 256 && group <= 2) || (d.d_head == 128 && (group <= 2 || group == 4));
+  static thread_local AttnLaunch L;
+  static thread_local SharedPrefixParams P;
+  // every launch is described before the first one is made: a call that is refused has done nothing
+  for (int pass = 0; pass < 2; ++pass)
+    for (int b0 = 0; b0 < batch; b0 += AT_MAX_SEQS) {
+      const int nb = batch - b0 < AT_MAX_SEQS ? batch - b0 : AT_MAX_SEQS;
+      int lo_all = INT32_MAX, hi_all = -1;
+      for (int i = 0; i < nb; ++i) {
+        const int qp = q_pos[b0 + i];
+        int lo = first_visible(qp, ls.window);
+        lo = (lo > prefix->first_pos ? lo : prefix->first_pos) - prefix->first_pos;
+        const int hi = qp < prefix->first_pos ? -1 : qp - prefix->first_pos < prefix->len ? qp - prefix->first_pos : prefix->len - 1;
+        P.lo[i] = lo;
+        P.hi[i] = hi;
+        if (prefix->len > 0 && hi >= lo) {
+          lo_all = lo < lo_all ? lo : lo_all;
+          hi_all = hi > hi_all ? hi : hi_all;
+        }
+      }
+      int pre[AT_MAX_SEQS];
+      P.splits = 0;
+      if (hi_all >= 0) {
+        P.rows = nb * group;
+        P.row_tiles = (P.rows + 127) / 128;
+        P.key0 = lo_all;
+        const int bk = shared_prefix_block(d.d_head), nt = shared_prefix_tiles(d.d_head, P.row_tiles);
+        P.n_blk = (hi_all - lo_all) / bk + 1;
+        // as many shares of the prefix as fill the SMs once, as far as blocks and the workspace's slots go
+        st = build_attn_launch(ctx, ls, b0, nb, q, q_pos, segs, n_segs, scale, out, nullptr, L);
+        if (st != KVD_OK) return st;
+        const int ctas = (P.row_tiles + nt - 1) / nt * d.n_kv_heads;
+        int splits = ctx->num_sms / ctas;
+        const int room = (ctx->max_parts - L.total_chunks) / nb;
+        splits = splits < P.n_blk ? splits : P.n_blk;
+        splits = splits < room ? splits : room;
+        if (room < 1) return KVD_ERR_CAPACITY;
+        P.splits = splits < 1 ? 1 : splits;
+      }
+      for (int i = 0; i < nb; ++i) pre[i] = P.splits;
+      st = build_attn_launch(ctx, ls, b0, nb, q, q_pos, segs, n_segs, scale, out, P.splits > 0 ? pre : nullptr, L, tails);
+      if (st != KVD_OK) return st;
+      if (pass == 0) continue;
+      if (P.splits > 0) {
+        P.q = L.q;
+        P.n_q = d.n_q_heads;
+        P.n_kv = d.n_kv_heads;
+        P.scale_log2e = L.scale_log2e;
+        P.part_o = ctx->part_o;
+        P.part_ml = ctx->part_ml;
+        P.max_parts = ctx->max_parts;
+        P.status = ctx->d_status;
+        P.timeout_ns = ctx->timeout_ns;
+        for (int i = 0; i < nb; ++i) P.slot[i] = L.seq[i].merge_base;
+        st = launch_shared_prefix(ctx, P, *prefix, d.d_head, group, stream);
+        if (st != KVD_OK) return st;
+      }
+      st = launch_attention(ctx, L, d.d_head, group, stream);
+      if (st != KVD_OK) return st;
+    }
+  return KVD_OK;
+}
+
+// Scores of a launch that weighs its keys, per query head: whole chunks over the visible span.
+static long long score_columns(const kvd_model_desc &d, int span) {
+  return span + 2ll * attn_chunk_keys(d.d_head, attn_iters_for_span(d.d_head, d.n_kv_heads, span));
+}
+
+extern "C" size_t kvd_weights_scratch_bytes(const kvd_model_desc *desc, int batch, int max_span) {
+  if (check_desc(desc) != KVD_OK || batch <= 0 || max_span <= 0) return 0;
+  const size_t seqs = batch < AT_MAX_SEQS ? batch : AT_MAX_SEQS;  // (a launch's; the next launch of a call reuses them)
+  return round_up(seqs * desc->n_q_heads * score_columns(*desc, max_span) * sizeof(float), 256);
+}
+
+extern "C" kvd_status kvd_decode_attention_weights(kvd_ctx *ctx, int layer, int batch, const void *q, const int32_t *q_pos,
+                                                   const kvd_kv_segment *segs, int n_segs, float scale, void *out,
+                                                   const float *weights_in, float *weights_out, int64_t weights_stride,
+                                                   int n_positions, void *scratch, size_t scratch_bytes, void *stream_) {
+  if (!ctx || batch < 0 || n_segs < 0 || n_segs > KVD_MAX_SEGMENTS) return KVD_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= ctx->desc.n_layers) return KVD_ERR_INVALID_ARG;
+  const LayerState &ls = ctx->layers[layer];
+  if (!ls.set) return KVD_ERR_STATE;
+  if (!ctx->part_o) return KVD_ERR_STATE;
+  if (ctx->dtype == KVD_DTYPE_F32) return KVD_ERR_UNSUPPORTED;
+  if (batch == 0) return KVD_OK;
+  if (!q || !q_pos || !out || !weights_out || !scratch || (n_segs > 0 && !segs)) return KVD_ERR_INVALID_ARG;
+  if (n_positions < 0 || weights_stride < n_positions) return KVD_ERR_INVALID_ARG;
+  if (n_positions > (1 << 30)) return KVD_ERR_CAPACITY;
+  if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return KVD_ERR_ALIGNMENT;
+  const kvd_model_desc &d = ctx->desc;
+  if (batch > d.max_batch) return KVD_ERR_CAPACITY;
+  const int group = d.n_q_heads / d.n_kv_heads;
+  kvd_status st = check_segments(ctx, batch, q_pos, segs, n_segs);
+  if (st != KVD_OK) return st;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  static thread_local AttnLaunch L;
+  // every launch is described before the first one is made: a call that is refused has done nothing
+  for (int pass = 0; pass < 2; ++pass)
+    for (int b0 = 0; b0 < batch; b0 += AT_MAX_SEQS) {
+      const int nb = batch - b0 < AT_MAX_SEQS ? batch - b0 : AT_MAX_SEQS;
+      st = build_attn_launch(ctx, ls, b0, nb, q, q_pos, segs, n_segs, scale, out, nullptr, L);
+      if (st != KVD_OK) return st;
+      long long columns = 0;
+      for (int i = 0; i < nb; ++i) {
+        const AttnSeq &S = L.seq[i];
+        if (S.n_chunks == 0) continue;
+        if (S.hi_pos >= n_positions) return KVD_ERR_CAPACITY;
+        const long long own = static_cast<long long>(S.n_chunks) * attn_chunk_keys(d.d_head, S.iters);
+        columns = own > columns ? own : columns;
+      }
+      if (static_cast<size_t>(nb) * d.n_q_heads * columns * sizeof(float) > scratch_bytes) return KVD_ERR_CAPACITY;
+      if (pass == 0) continue;
+      L.scores = static_cast<float *>(scratch);
+      L.score_stride = columns;
+      AttnWeigh W = {};
+      W.in = weights_in ? weights_in + static_cast<size_t>(b0) * weights_stride : nullptr;
+      W.out = weights_out + static_cast<size_t>(b0) * weights_stride;
+      W.stride = weights_stride;
+      W.n_positions = n_positions;
+      st = launch_attention_weights(ctx, L, d.d_head, group, W, stream);
+      if (st != KVD_OK) return st;
+    }
   return KVD_OK;
 }
 

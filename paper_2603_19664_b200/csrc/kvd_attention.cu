@@ -118,7 +118,9 @@ __device__ __forceinline__ const __nv_bfloat16 *lane_ptr(const __nv_bfloat16 *p,
 // a few thousand keys), where nothing else on the SM hides a load's latency: the loads of both iterations are
 // issued before the query is fetched and before anything is computed, so a CTA pays one memory round trip
 // instead of three.  The arithmetic and its order are the same, hence the same bits.
-template <int D_HEAD, int G, int NSEQ, int DT = 0, bool ALLIN = false>
+// WEIGH: the scores are stored as well, for the keys' weights (attn_weigh_cta): 4 bytes per key and query head beside the
+// 4 d_head that K and V of a key are.
+template <int D_HEAD, int G, int NSEQ, int DT = 0, bool ALLIN = false, bool WEIGH = false>
 __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_attn_split_kernel(const __grid_constant__ AttnLaunchT<NSEQ> P) {
   constexpr int LPK = D_HEAD / 8;         // lanes per key
   constexpr int KPL = 32 / LPK;           // keys per warp-wide load
@@ -217,7 +219,7 @@ __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_at
   };
 
   // scores, online softmax and weighted values for the 8 keys of one iteration
-  auto compute = [&](const uint4 (&kr)[U], const uint4 (&vr)[U], uint32_t vmask) {
+  auto compute = [&](int it, const uint4 (&kr)[U], const uint4 (&vr)[U], uint32_t vmask) {
     // ---- scores: per-lane partial dot products (one key unpacked at a time), then the transposing
     // reduction
     float part[G][U];
@@ -244,6 +246,10 @@ __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_at
     for (int g = 0; g < G; ++g) {
       float sc = reduce8_transposed<LPK>(part[g], lig);
       sc = my_valid ? sc : -CUDART_INF_F;
+      if constexpr (WEIGH) {
+        if ((lig & (LPK / 8 - 1)) == 0 && KVD_BOUNDS_OK(chunk * chunk_keys + chunk_keys <= P.score_stride, P.status))
+          P.scores[(static_cast<size_t>(si) * P.n_q + kvh * G + g) * P.score_stride + chunk * chunk_keys + ((it * AT_WARPS + warp) * KPL + grp) * U + my_slot] = sc;
+      }
       float bmax = sc;
       bmax = fmaxf(bmax, __shfl_xor_sync(0xffffffffu, bmax, LPK / 2));
       bmax = fmaxf(bmax, __shfl_xor_sync(0xffffffffu, bmax, LPK / 4));
@@ -286,8 +292,8 @@ __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_at
   };
   // a warp none of whose keys is visible has nothing to add (warp-uniform test: the reductions
   // inside compute() use the whole warp)
-  auto step = [&](const uint4 (&kr)[U], const uint4 (&vr)[U], uint32_t vmask) {
-    if (__any_sync(0xffffffffu, vmask != 0u)) compute(kr, vr, vmask);
+  auto step = [&](int it, const uint4 (&kr)[U], const uint4 (&vr)[U], uint32_t vmask) {
+    if (__any_sync(0xffffffffu, vmask != 0u)) compute(it, kr, vr, vmask);
   };
 
   if constexpr (ALLIN) {
@@ -302,8 +308,8 @@ __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_at
       issue_any(1, kb, vb, mb);
     }
     load_query();
-    step(ka, va, ma);
-    step(kb, vb, mb);
+    step(0, ka, va, ma);
+    step(1, kb, vb, mb);
   } else {
     // One buffer of loads per iteration; latency is hidden by the other 15 warps resident on the SM
     // (the kernel is capped at 128 registers so that four CTAs fit), which measured faster than
@@ -314,7 +320,7 @@ __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_at
     for (int it = 0; it < S.iters; ++it) {
       if (whole.linear) issue_linear(it, ka, va, ma);
       else issue_any(it, ka, va, ma);
-      step(ka, va, ma);
+      step(it, ka, va, ma);
     }
   }
 
@@ -413,7 +419,7 @@ __device__ __forceinline__ void mma_x16_m16n8k8(float (&c)[4], uint32_t a0, uint
                  : "r"(a0), "r"(a1), "r"(b0));
 }
 
-template <int D_HEAD, int G, int NSEQ, int DT = 0, int SLOTS = 3>
+template <int D_HEAD, int G, int NSEQ, int DT = 0, int SLOTS = 3, bool WEIGH = false>
 __global__ void __launch_bounds__(AT_THREADS, SLOTS == 3 ? AT_CTAS_PER_SM : 3)
     kvd_attn_split_mma_kernel(const __grid_constant__ AttnLaunchT<NSEQ> P) {
   static_assert(G >= 1 && G <= 8 && D_HEAD <= 128, "query heads are the 8 columns of the second product");
@@ -540,6 +546,11 @@ __global__ void __launch_bounds__(AT_THREADS, SLOTS == 3 ? AT_CTAS_PER_SM : 3)
       // thread (g8, t): head g8, keys 2t and 2t+1 of the block
       const float s0 = ((vis >> (8 * b + 2 * t)) & 1u) ? sc[b][0] * P.scale_log2e : -CUDART_INF_F;
       const float s1 = ((vis >> (8 * b + 2 * t + 1)) & 1u) ? sc[b][1] * P.scale_log2e : -CUDART_INF_F;
+      if constexpr (WEIGH) {
+        const int at = chunk * chunk_keys + (it * AT_WARPS + warp) * WARP_KEYS + 8 * b + 2 * t;  // (even, and so is the stride)
+        if (g8 < G && KVD_BOUNDS_OK(at + 2 <= P.score_stride, P.status))
+          *reinterpret_cast<float2 *>(P.scores + (static_cast<size_t>(si) * P.n_q + kvh * G + g8) * P.score_stride + at) = make_float2(s0, s1);
+      }
       float bmax = fmaxf(s0, s1);
       bmax = fmaxf(bmax, __shfl_xor_sync(0xffffffffu, bmax, 1));
       bmax = fmaxf(bmax, __shfl_xor_sync(0xffffffffu, bmax, 2));
@@ -651,8 +662,7 @@ __global__ void __launch_bounds__(AT_THREADS, SLOTS == 3 ? AT_CTAS_PER_SM : 3)
 // sequence, of which there are AT_TAIL_KEYS at most, while the others (one fewer at most) fetch its partials; the two are put
 // together at the end.  A sequence without such keys is merged as in the other launches, by all warps.
 template <int D_HEAD, int G, int NSEQ, int DT, int GH, bool TAIL>
-__global__ void __launch_bounds__(AT_MERGE_THREADS)
-    kvd_attn_merge_kernel(const __grid_constant__ AttnLaunchT<NSEQ> P) {
+__device__ __forceinline__ void attn_merge_cta(const AttnLaunchT<NSEQ> &P, int block) {
   constexpr int SLICES = D_HEAD / AT_MERGE_SLICE;
   constexpr int PF = attn_merge_group(G);
   // of every warp of the CTA: outputs [GH][AT_MERGE_SLICE] and sums [GH] (as much as the launch's warps need: the kernel's
@@ -662,17 +672,13 @@ __global__ void __launch_bounds__(AT_MERGE_THREADS)
   float (*s_o)[GH][AT_MERGE_SLICE] = reinterpret_cast<float (*)[GH][AT_MERGE_SLICE]>(at_merge_smem);
   float (*s_l)[GH] = reinterpret_cast<float (*)[GH]>(at_merge_smem + blockDim.x / 32 * GH * AT_MERGE_SLICE);
   float *s_max = at_merge_smem + blockDim.x / 32 * GH * (AT_MERGE_SLICE + 1);  // TAIL: maxima of the partials [GH], of the keys [GH]
-  const int slice = blockIdx.x % SLICES;
-  const int head_slot = blockIdx.x / SLICES;
+  const int slice = block % SLICES;
+  const int head_slot = block / SLICES;
   const int si = head_slot / (P.n_q / GH), head0 = head_slot % (P.n_q / GH) * GH;  // sequence, first query head
   const AttnSeq &S = P.seq[si];
   const bool tail = TAIL && attn_tail(S);
   const int max_warps = AT_MERGE_WARPS - (tail ? 1 : 0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  grid_launch_dependents();
-  // wait until the preceding grid in the stream (the streaming kernel) has completed and its
-  // partials are visible
-  grid_dependency_wait();
 
   // (checking build: the slots to merge lie inside the partial arrays; otherwise nothing is merged)
   const int count = KVD_BOUNDS_OK(S.merge_base >= 0 && S.merge_base + S.merge_count <= P.max_parts, P.status) ? S.merge_count : 0;
@@ -835,6 +841,93 @@ __global__ void __launch_bounds__(AT_MERGE_THREADS)
     else reinterpret_cast<__half *>(P.out)[oi] = __float2half_rn(r);
   }
 }
+template <int D_HEAD, int G, int NSEQ, int DT, int GH, bool TAIL>
+__global__ void __launch_bounds__(AT_MERGE_THREADS)
+    kvd_attn_merge_kernel(const __grid_constant__ AttnLaunchT<NSEQ> P) {
+  grid_launch_dependents();
+  // wait until the preceding grid in the stream (the streaming kernel) has completed and its
+  // partials are visible
+  grid_dependency_wait();
+  attn_merge_cta<D_HEAD, G, NSEQ, DT, GH, TAIL>(P, static_cast<int>(blockIdx.x));
+}
+
+// What every key weighed: w_j <- w_j + sum_h 2^(s_hj - m_h) / l_h over all query heads (Eq. 6's weights, which only exist
+// once a row's maximum and sum are known), from the scores that the streaming kernel stored in log2 units and the partials'
+// maxima and sums.  A CTA takes a run of positions of one sequence, two neighbours per thread; it puts the heads' statistics
+// together itself, so that it need not wait for the merge, whose launch it shares.  Heads are added in ascending order.  A
+// position that the query does not see or that nobody holds keeps its weight; a head whose keys all score minus infinity
+// adds nothing.
+template <int NSEQ>
+__device__ __forceinline__ void attn_weigh_cta(const AttnLaunchT<NSEQ> &P, const AttnWeigh &W, int block) {
+  extern __shared__ float at_merge_smem[];  // per head: -(m + log2 l), or minus infinity for a head that adds nothing
+  const int si = block / W.tiles, pos0 = block % W.tiles * (2 * static_cast<int>(blockDim.x)), p = pos0 + 2 * static_cast<int>(threadIdx.x);
+  const AttnSeq &S = P.seq[si];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = static_cast<int>(blockDim.x) >> 5;
+  const bool some = S.n_chunks > 0 && pos0 <= S.hi_pos && ends_by(pos0, 2 * static_cast<int>(blockDim.x), S.lo_pos - 1) == false;
+  const int count = KVD_BOUNDS_OK(S.slot_base >= 0 && S.slot_base + S.n_chunks <= P.max_parts, P.status) ? S.n_chunks : 0;
+  if (some) {
+    const float2 *ml0 = reinterpret_cast<const float2 *>(P.part_ml) + static_cast<size_t>(S.merge_base) * P.n_q;
+    const int n = S.merge_count < count ? S.merge_count : count;
+    for (int h = warp; h < P.n_q; h += warps) {
+      float2 ml[6];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) ml[i] = lane + 32 * i < n ? __ldcg(ml0 + static_cast<size_t>(lane + 32 * i) * P.n_q + h) : make_float2(-CUDART_INF_F, 0.f);
+      float m = -CUDART_INF_F, l = 0.f;
+#pragma unroll
+      for (int i = 0; i < 6; ++i) m = fmaxf(m, ml[i].x);
+      for (int c = lane + 192; c < n; c += 32) m = fmaxf(m, __ldcg(ml0 + static_cast<size_t>(c) * P.n_q + h).x);
+#pragma unroll
+      for (int k = 16; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+      const float mu = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < 6; ++i) l = fmaf(exp2f(ml[i].x - mu), ml[i].y, l);
+      for (int c = lane + 192; c < n; c += 32) {
+        const float2 v = __ldcg(ml0 + static_cast<size_t>(c) * P.n_q + h);
+        l = fmaf(exp2f(v.x - mu), v.y, l);
+      }
+#pragma unroll
+      for (int k = 16; k >= 1; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+      if (lane == 0) at_merge_smem[h] = l == 0.f ? -CUDART_INF_F : -(mu + log2f(l));
+    }
+  }
+  __syncthreads();
+  if (p >= W.n_positions) return;
+  float w0 = 0.f, w1 = 0.f;
+  if (some) {
+    const bool in0 = p >= S.lo_pos && p <= S.hi_pos, in1 = p + 1 >= S.lo_pos && p < S.hi_pos;
+    bool see0 = false, see1 = false;
+#pragma unroll
+    for (int sg = 0; sg < KVD_MAX_SEGMENTS; ++sg) {
+      see0 |= in0 && segment_holds(S.first[sg], S.len[sg], p, 1);
+      see1 |= in1 && segment_holds(S.first[sg], S.len[sg], p + 1, 1);
+    }
+    if (see0 || see1) {
+      const float *sc = P.scores + static_cast<size_t>(si) * P.n_q * P.score_stride + (p - S.chunk0_pos);
+#pragma unroll 8
+      for (int h = 0; h < P.n_q; ++h) {
+        const float2 s = __ldcg(reinterpret_cast<const float2 *>(sc + static_cast<size_t>(h) * P.score_stride));
+        const float nl = at_merge_smem[h];
+        w0 += exp2f(s.x + nl);
+        w1 += exp2f(s.y + nl);
+      }
+      if (!see0) w0 = 0.f;
+      if (!see1) w1 = 0.f;
+    }
+  }
+  const size_t at = static_cast<size_t>(si) * W.stride + p;
+  W.out[at] = (W.in ? W.in[at] : 0.f) + w0;
+  if (p + 1 < W.n_positions) W.out[at + 1] = (W.in ? W.in[at + 1] : 0.f) + w1;
+}
+// The merge of a launch that weighs its keys: merge CTAs first, then those of the weights.
+template <int D_HEAD, int G, int NSEQ, int DT, int GH>
+__global__ void __launch_bounds__(AT_MERGE_THREADS)
+    kvd_attn_merge_weigh_kernel(const __grid_constant__ AttnLaunchT<NSEQ> P, const __grid_constant__ AttnWeigh W) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int merges = static_cast<int>(gridDim.x) - P.n_seqs * W.tiles;
+  if (static_cast<int>(blockIdx.x) < merges) attn_merge_cta<D_HEAD, G, NSEQ, DT, GH, false>(P, static_cast<int>(blockIdx.x));
+  else attn_weigh_cta<NSEQ>(P, W, static_cast<int>(blockIdx.x) - merges);
+}
 
 // dynamic shared memory of the kernel and its one-time opt-in (sizes above 48 KB need it); the device's SMs
 template <int D_HEAD, int G>
@@ -842,7 +935,7 @@ struct AttnSmem {
   static constexpr int NPART = AT_WARPS * (32 / (D_HEAD / 8));
   static constexpr int BYTES = NPART * G * (D_HEAD + 2) * 4;
 };
-template <int D_HEAD, int G, int NSEQ, int DT>
+template <int D_HEAD, int G, int NSEQ, int DT, bool WEIGH>
 static cudaError_t attn_configure(int *num_sms) {
   static std::atomic<int> sms[64] = {};  // 0: not configured yet
   int dev = 0;
@@ -851,16 +944,16 @@ static cudaError_t attn_configure(int *num_sms) {
   *num_sms = sms[dev & 63].load(std::memory_order_acquire);
   if (*num_sms == 0) {
     if constexpr (G >= 3 && D_HEAD <= 128) {
-      e = cudaFuncSetAttribute(kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, AT_WARPS * 3 * AT_PIECE);
+      e = cudaFuncSetAttribute(kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 3, WEIGH>, cudaFuncAttributeMaxDynamicSharedMemorySize, AT_WARPS * 3 * AT_PIECE);
       if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, AT_WARPS * 4 * AT_PIECE);
+        e = cudaFuncSetAttribute(kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 4, WEIGH>, cudaFuncAttributeMaxDynamicSharedMemorySize, AT_WARPS * 4 * AT_PIECE);
       if (e != cudaSuccess) return e;
     } else {
-      e = cudaFuncSetAttribute(kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      e = cudaFuncSetAttribute(kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT, false, WEIGH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                AttnSmem<D_HEAD, G>::BYTES);
       if (e != cudaSuccess) return e;
       if constexpr (G <= 2) {
-        e = cudaFuncSetAttribute(kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT, true>,
+        e = cudaFuncSetAttribute(kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT, true, WEIGH>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize, AttnSmem<D_HEAD, G>::BYTES);
         if (e != cudaSuccess) return e;
       }
@@ -871,11 +964,11 @@ static cudaError_t attn_configure(int *num_sms) {
   }
   return cudaSuccess;
 }
-// the two launches of a decode step: stream + partials, then merge
-template <int D_HEAD, int G, int NSEQ, int DT = 0>
-static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t stream) {
+// the two launches of a decode step: stream + partials, then merge (WEIGH: and the keys' weights, `weigh` says where)
+template <int D_HEAD, int G, int NSEQ, int DT = 0, bool WEIGH = false>
+static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t stream, const AttnWeigh *weigh = nullptr) {
   int num_sms = 0;
-  cudaError_t e = attn_configure<D_HEAD, G, NSEQ, DT>(&num_sms);
+  cudaError_t e = attn_configure<D_HEAD, G, NSEQ, DT, WEIGH>(&num_sms);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
@@ -901,18 +994,18 @@ static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t str
     if constexpr (G >= 3 && D_HEAD <= 128) {
       const bool few = S.total_chunks * S.n_kv <= num_sms * 3;  // all of the grid at once with four pieces per warp
       cfg.dynamicSmemBytes = AT_WARPS * (few ? 4 : 3) * AT_PIECE;
-      if (few) e = cudaLaunchKernelEx(&cfg, kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 4>, S);
-      else e = cudaLaunchKernelEx(&cfg, kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 3>, S);
+      if (few) e = cudaLaunchKernelEx(&cfg, kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 4, WEIGH>, S);
+      else e = cudaLaunchKernelEx(&cfg, kvd_attn_split_mma_kernel<D_HEAD, G, NSEQ, DT, 3, WEIGH>, S);
     } else {
       cfg.dynamicSmemBytes = AttnSmem<D_HEAD, G>::BYTES;
       // at most two CTAs per SM, every chunk two iterations long: the variant that issues all loads at once
       bool allin = G <= 2 && S.total_chunks * S.n_kv <= num_sms * 2;
       for (int i = 0; i < S.n_seqs; ++i) allin = allin && (S.seq[i].n_chunks == 0 || S.seq[i].iters == 2);
       if constexpr (G <= 2) {
-        if (allin) e = cudaLaunchKernelEx(&cfg, kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT, true>, S);
-        else e = cudaLaunchKernelEx(&cfg, kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT>, S);
+        if (allin) e = cudaLaunchKernelEx(&cfg, kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT, true, WEIGH>, S);
+        else e = cudaLaunchKernelEx(&cfg, kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT, false, WEIGH>, S);
       } else {
-        e = cudaLaunchKernelEx(&cfg, kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT>, S);
+        e = cudaLaunchKernelEx(&cfg, kvd_attn_split_kernel<D_HEAD, G, NSEQ, DT, false, WEIGH>, S);
       }
     }
     if (e != cudaSuccess) return e;
@@ -936,6 +1029,14 @@ static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t str
   };
   auto merge_by = [&](auto heads_c) {
     constexpr int GH = decltype(heads_c)::value;
+    if constexpr (WEIGH) {
+      AttnWeigh W = *weigh;
+      W.tiles = (W.n_positions + 64 * merge_warps - 1) / (64 * merge_warps);
+      const size_t merge_smem = (merge_warps * (AT_MERGE_SLICE + 1) + 2) * GH * sizeof(float), weigh_smem = S.n_q * sizeof(float);
+      cfg.gridDim = dim3(S.n_seqs * ((S.n_q / GH) * (D_HEAD / AT_MERGE_SLICE) + W.tiles), 1, 1);
+      cfg.dynamicSmemBytes = merge_smem > weigh_smem ? merge_smem : weigh_smem;
+      return cudaLaunchKernelEx(&cfg, kvd_attn_merge_weigh_kernel<D_HEAD, G, NSEQ, DT, GH>, S, W);
+    }
     if constexpr (TAILS) {
       if (S.tail) return merge(kvd_attn_merge_kernel<D_HEAD, G, NSEQ, DT, GH, true>, GH);
     }
@@ -952,8 +1053,14 @@ static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t str
   return merge_by(std::integral_constant<int, G>());
 }
 
+// This file is compiled twice, side by side: as it is, and by kvd_attention_weights.cu for the launches that weigh their keys.
+#ifdef KVD_ATTENTION_WEIGHTS
+constexpr bool ATTN_WEIGH = true;
+#else
+constexpr bool ATTN_WEIGH = false;
+#endif
 template <int D_HEAD, int G, int NSEQ>
-static kvd_status launch_attn_impl(kvd_ctx *ctx, const AttnLaunch &L, cudaStream_t stream) {
+static kvd_status launch_attn_impl(kvd_ctx *ctx, const AttnLaunch &L, cudaStream_t stream, const AttnWeigh *weigh) {
   if (L.n_seqs > 0) {
     static thread_local AttnLaunchT<NSEQ> S;
     static_cast<AttnLaunchHead &>(S) = static_cast<const AttnLaunchHead &>(L);
@@ -961,8 +1068,8 @@ static kvd_status launch_attn_impl(kvd_ctx *ctx, const AttnLaunch &L, cudaStream
     // straight behind the projection of the new tokens (attn_launch_pair says why; a second launch of the same call is not)
     S.early = ctx->few_rows.directly_before(ctx->launches, stream);
     // fp16 contexts (kvd_set_dtype): the same kernels reading and writing fp16
-    cudaError_t e = ctx->dtype == 1 ? attn_launch_pair<D_HEAD, G, NSEQ, 1>(S, stream)
-                                    : attn_launch_pair<D_HEAD, G, NSEQ, 0>(S, stream);
+    cudaError_t e = ctx->dtype == 1 ? attn_launch_pair<D_HEAD, G, NSEQ, 1, ATTN_WEIGH>(S, stream, weigh)
+                                    : attn_launch_pair<D_HEAD, G, NSEQ, 0, ATTN_WEIGH>(S, stream, weigh);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "launch attention");
     ctx->launches += L.total_chunks > 0 ? 2 : 1;
   }
@@ -970,34 +1077,45 @@ static kvd_status launch_attn_impl(kvd_ctx *ctx, const AttnLaunch &L, cudaStream
 }
 
 template <int D_HEAD, int G>
-static kvd_status launch_attn_nseq(kvd_ctx *ctx, const AttnLaunch &L, cudaStream_t stream) {
-  if (L.n_seqs <= 4) return launch_attn_impl<D_HEAD, G, 4>(ctx, L, stream);
-  return launch_attn_impl<D_HEAD, G, AT_MAX_SEQS>(ctx, L, stream);
+static kvd_status launch_attn_nseq(kvd_ctx *ctx, const AttnLaunch &L, cudaStream_t stream, const AttnWeigh *weigh) {
+  if (L.n_seqs <= 4) return launch_attn_impl<D_HEAD, G, 4>(ctx, L, stream, weigh);
+  return launch_attn_impl<D_HEAD, G, AT_MAX_SEQS>(ctx, L, stream, weigh);
 }
 
 template <int D_HEAD>
-static kvd_status launch_attn_group(kvd_ctx *ctx, const AttnLaunch &L, int group, cudaStream_t stream) {
+static kvd_status launch_attn_group(kvd_ctx *ctx, const AttnLaunch &L, int group, cudaStream_t stream, const AttnWeigh *weigh) {
   switch (group) {
-    case 1: return launch_attn_nseq<D_HEAD, 1>(ctx, L, stream);
-    case 2: return launch_attn_nseq<D_HEAD, 2>(ctx, L, stream);
-    case 3: return launch_attn_nseq<D_HEAD, 3>(ctx, L, stream);
-    case 4: return launch_attn_nseq<D_HEAD, 4>(ctx, L, stream);
-    case 8: return launch_attn_nseq<D_HEAD, 8>(ctx, L, stream);
+    case 1: return launch_attn_nseq<D_HEAD, 1>(ctx, L, stream, weigh);
+    case 2: return launch_attn_nseq<D_HEAD, 2>(ctx, L, stream, weigh);
+    case 3: return launch_attn_nseq<D_HEAD, 3>(ctx, L, stream, weigh);
+    case 4: return launch_attn_nseq<D_HEAD, 4>(ctx, L, stream, weigh);
+    case 8: return launch_attn_nseq<D_HEAD, 8>(ctx, L, stream, weigh);
     default: return KVD_ERR_SHAPE;
   }
 }
 
-kvd_status launch_attention(kvd_ctx *ctx, const AttnLaunch &L, int d_head, int group, cudaStream_t stream) {
+static kvd_status launch_attn(kvd_ctx *ctx, const AttnLaunch &L, int d_head, int group, cudaStream_t stream, const AttnWeigh *weigh) {
   switch (d_head) {
-    case 64: return launch_attn_group<64>(ctx, L, group, stream);
-    case 128: return launch_attn_group<128>(ctx, L, group, stream);
-    case 256: return launch_attn_group<256>(ctx, L, group, stream);
+    case 64: return launch_attn_group<64>(ctx, L, group, stream, weigh);
+    case 128: return launch_attn_group<128>(ctx, L, group, stream, weigh);
+    case 256: return launch_attn_group<256>(ctx, L, group, stream, weigh);
     default: return KVD_ERR_SHAPE;
   }
 }
+
+#ifdef KVD_ATTENTION_WEIGHTS
+kvd_status launch_attention_weights(kvd_ctx *ctx, const AttnLaunch &L, int d_head, int group, const AttnWeigh &weigh, cudaStream_t stream) {
+  return launch_attn(ctx, L, d_head, group, stream, &weigh);
+}
+#else
+kvd_status launch_attention(kvd_ctx *ctx, const AttnLaunch &L, int d_head, int group, cudaStream_t stream) {
+  return launch_attn(ctx, L, d_head, group, stream, nullptr);
+}
+#endif
 
 }  // namespace kvd
 
+#ifndef KVD_ATTENTION_WEIGHTS
 // ------------------------------------------------------------------------------------------------
 // kvd_decode_attention_static: decode attention for callers that cannot allocate device memory.
 //
@@ -1170,3 +1288,4 @@ extern "C" kvd_status kvd_decode_attention_static(int n_q_heads, int n_kv_heads,
     default: return static_launch_d<256>(L, group, stream);
   }
 }
+#endif  // KVD_ATTENTION_WEIGHTS

@@ -1,0 +1,420 @@
+// Eviction from a cache by accumulated weight (include/kvd.h, kvd_cache_evict).
+//
+// Of the len slots of a sequence the `keep` largest stay, in the order (protected, weight, lower slot first).  Both parts of
+// that order fit one 32-bit key, larger is better: the weight's bits mapped so that unsigned order is numeric order (a NaN
+// counts as minus infinity, -0 as +0), and above all of them one value for protected slots.  The keep-th largest key T is
+// found digit by digit (11, 11 and 10 bits from the top): a histogram of the keys that agree with T so far, and in it the
+// digit at which the count from above passes what is still wanted.  Slots above T stay, and of those equal to T as many of
+// the lowest as are wanted.
+//
+// One cluster per sequence, its slots dealt out in contiguous runs that stay in shared memory, so that memory is read once.
+// Histograms of the CTAs are added up in the shared memory of rank 0 (integer additions: their order changes nothing), every
+// CTA scans the sum itself; ranks among kept, evicted and moved slots are prefix counts, over threads, warps and CTAs.
+//
+// Slots below `keep` that stay keep their place; the r-th evicted slot below `keep` (a hole) receives the r-th kept slot
+// from `keep` on (a mover).  So an eviction in place moves as few keys as possible, and no key is read that the same call
+// overwrites: sources lie at `keep` and above, destinations below.  The second kernel copies the keys' rows.
+#include <math_constants.h>
+#include <string.h>
+
+#include "kvd_internal.h"
+#include "kvd_ptx.cuh"
+
+namespace kvd {
+
+constexpr int EV_THREADS = 1024;
+constexpr int EV_WARPS = EV_THREADS / 32;
+constexpr int EV_BINS = 2048;
+constexpr int EV_MAX_CTAS = 8;                    // a portable cluster
+constexpr int EV_CTA_SLOTS = KVD_MAX_EVICT_SLOTS / EV_MAX_CTAS;
+constexpr int EV_RUN = 1024;                      // slots that one CTA is enough for
+constexpr uint32_t EV_PROTECTED = 0xffffffffu;    // above the key of plus infinity, 0xff800000
+constexpr uint32_t EV_GONE = 0x80000000u, EV_MOVES = 0x40000000u;
+constexpr int EV_MAX_SEQS = 64;
+constexpr int EV_ROW_THREADS = 256;
+
+struct EvictParams {
+  const float *weights;
+  const int32_t *positions;  // or null: slot j holds position j
+  float *weights_out;        // or null
+  int32_t *positions_out;    // or null
+  int32_t *slots_out, *evicted_out;
+  long long cap_in, cap_out, evicted_stride;  // slots per sequence
+  int keep, protect_below, run;  // run: slots per CTA of the cluster
+  const uint4 *k, *v;
+  uint4 *k_out, *v_out;
+  long long row_in, row_out;  // 16-byte chunks between rows
+  int row_chunks, rows_per_cta;
+  int *status;
+  int len[EV_MAX_SEQS], protect_from[EV_MAX_SEQS];
+};
+
+struct EvictShared {
+  uint32_t hist[3][EV_BINS];    // this CTA's counts, by pass
+  uint32_t sum[3][EV_BINS];     // rank 0: the cluster's, added up by remote atomics
+  uint32_t warp_sum[EV_WARPS], part[2][EV_WARPS];
+  uint32_t digit, above;        // found in the current pass
+  uint32_t count[2];            // of this CTA's run: slots equal to T; evicted ones and movers
+};
+
+__device__ __forceinline__ uint32_t evict_key(float w) {
+  w = w == w ? w + 0.0f : -CUDART_INF_F;
+  const uint32_t u = __float_as_uint(w);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_cluster_u32(uint32_t addr, uint32_t v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+__global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const __grid_constant__ EvictParams P, int ctas) {
+  extern __shared__ __align__(16) uint8_t ev_smem[];
+  EvictShared &S = *reinterpret_cast<EvictShared *>(ev_smem);
+  uint32_t *ev_keys = reinterpret_cast<uint32_t *>(ev_smem + sizeof(EvictShared));  // [run], and the slots' positions behind them
+  int32_t *ev_pos = reinterpret_cast<int32_t *>(ev_keys + P.run);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = ctas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int b = static_cast<int>(blockIdx.x) / ctas;
+  const int len = P.len[b], keep = P.keep < len ? P.keep : len;
+  const int slot0 = rank * P.run, n = max(0, min(P.run, len - slot0));
+  auto all_sync = [&]() {
+    if (ctas > 1) cluster_sync_all();
+    else __syncthreads();
+  };
+  auto remote = [&](const void *p, int r) { return map_to_cta(smem_u32(p), static_cast<uint32_t>(r)); };  // (of a cluster)
+  auto clear = [&]() {
+    for (int i = tid; i < EV_BINS; i += EV_THREADS) {
+      S.hist[0][i] = S.hist[1][i] = S.hist[2][i] = 0u;
+      S.sum[0][i] = S.sum[1][i] = S.sum[2][i] = 0u;
+    }
+  };
+  clear();
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const float *w = P.weights + b * P.cap_in;
+  const int32_t *pos = P.positions ? P.positions + b * P.cap_in : nullptr;
+  const int from = P.protect_from[b];
+  auto is_protected = [&](int p) { return p < P.protect_below || p >= from; };
+  all_sync();  // histograms are clear everywhere
+  for (int i = tid; i < n; i += EV_THREADS) {
+    const int p = pos ? pos[slot0 + i] : slot0 + i;
+    const uint32_t key = is_protected(p) ? EV_PROTECTED : evict_key(w[slot0 + i]);
+    ev_keys[i] = key;
+    ev_pos[i] = p;
+    if (keep < len) atomicAdd(&S.hist[0][key >> 21], 1u);
+  }
+  // ---- T: the keep-th largest key; need: how many of the slots equal to it stay
+  uint32_t T, need;
+  auto select = [&]() {
+    T = 0u;
+    need = static_cast<uint32_t>(keep);
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      uint32_t *hist = S.hist[pass];
+      __syncthreads();
+      uint32_t *sum = S.sum[pass];
+      if (ctas > 1) {
+        const uint32_t dst = remote(sum, 0);
+        for (int i = tid; i < EV_BINS; i += EV_THREADS)
+          if (hist[i] != 0u) add_cluster_u32(dst + 4 * i, hist[i]);
+        cluster_sync_all();
+      }
+      // counts from the top: thread t holds bins 2047 - 2t and 2046 - 2t
+      uint32_t c0, c1;
+      if (ctas > 1) {
+        const uint32_t src = remote(sum, 0);
+        c0 = ld_cluster_u32(src + 4 * (EV_BINS - 1 - 2 * tid));
+        c1 = ld_cluster_u32(src + 4 * (EV_BINS - 2 - 2 * tid));
+      } else {
+        c0 = hist[EV_BINS - 1 - 2 * tid];
+        c1 = hist[EV_BINS - 2 - 2 * tid];
+      }
+      uint32_t incl = c0 + c1;
+#pragma unroll
+      for (int k = 1; k < 32; k <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, incl, k);
+        if (lane >= k) incl += o;
+      }
+      if (lane == 31) S.warp_sum[warp] = incl;
+      __syncthreads();
+      uint32_t before = 0;
+      {
+        const uint32_t v = lane < warp ? S.warp_sum[lane] : 0u;
+        before = __reduce_add_sync(0xffffffffu, v);
+      }
+      const uint32_t a0 = before + incl - c0 - c1, a1 = a0 + c0, a2 = a1 + c1;  // keys above either bin, and through both
+      if (a0 < need && need <= a1) {
+        S.digit = EV_BINS - 1 - 2 * tid;
+        S.above = a0;
+      } else if (a1 < need && need <= a2) {
+        S.digit = EV_BINS - 2 - 2 * tid;
+        S.above = a1;
+      }
+      __syncthreads();
+      T |= S.digit << shift;
+      need -= S.above;
+      if (pass < 2) {
+        const int next = pass == 0 ? 10 : 0;
+        const uint32_t mask = pass == 0 ? 0x7ffu : 0x3ffu;
+        uint32_t *nh = S.hist[pass + 1];
+        for (int i = tid; i < n; i += EV_THREADS) {
+          const uint32_t key = ev_keys[i];
+          if ((key >> shift) == (T >> shift)) atomicAdd(&nh[(key >> next) & mask], 1u);
+        }
+      }
+    }
+  };
+  T = need = 0u;
+  if (keep < len && keep > 0) {
+    select();
+    if (T == EV_PROTECTED) {
+      // Protected slots alone reach `keep`: once more among them, by their weights, with all others below minus infinity.
+      all_sync();
+      clear();
+      all_sync();
+      for (int i = tid; i < n; i += EV_THREADS) {
+        const uint32_t key = is_protected(ev_pos[i]) ? evict_key(w[slot0 + i]) : 0u;
+        ev_keys[i] = key;
+        atomicAdd(&S.hist[0][key >> 21], 1u);
+      }
+      select();
+    }
+  }
+  __syncthreads();
+  // ---- ranks.  Thread t owns the slots [t * per, (t + 1) * per) of the run, so that prefix counts over threads are in slot
+  // order.  A slot's key gives way to what becomes of it: its own index (stays), EV_MOVES | rank, EV_GONE | rank.
+  const int per = (n + EV_THREADS - 1) / EV_THREADS;
+  const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  auto block_excl = [&](uint32_t mine, uint32_t (&warp_part)[EV_WARPS], uint32_t *total) {  // counts of the threads before this one
+    uint32_t incl = mine;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+      const uint32_t o = __shfl_up_sync(0xffffffffu, incl, k);
+      if (lane >= k) incl += o;
+    }
+    if (lane == 31) warp_part[warp] = incl;
+    __syncthreads();
+    const uint32_t v = warp_part[lane];
+    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u);
+    *total = __reduce_add_sync(0xffffffffu, v);
+    return before + incl - mine;
+  };
+  // above T, or one of the lowest `need` equal to it (rank: of those before it)
+  auto stays = [&](uint32_t key, uint32_t &rank_of_equal) { return keep == len || (keep > 0 && (key > T || (key == T && rank_of_equal++ < need))); };
+  uint32_t equal = 0, total;
+  for (int i = i0; i < i1; ++i) equal += ev_keys[i] == T;
+  uint32_t equal_rank = block_excl(equal, S.part[0], &total);
+  if (ctas > 1) {
+    if (tid == 0) S.count[0] = total;
+    cluster_sync_all();
+    for (int r = 0; r < rank; ++r) equal_rank += ld_cluster_u32(remote(&S.count[0], r));
+  }
+  uint32_t both = 0;  // evicted slots, and movers in the upper half (a run has fewer than 2^16 slots)
+  {
+    uint32_t er = equal_rank;
+    for (int i = i0; i < i1; ++i) both += !stays(ev_keys[i], er) ? 1u : slot0 + i >= keep ? 0x10000u : 0u;
+  }
+  both = block_excl(both, S.part[1], &total);
+  uint32_t gone = both & 0xffffu, moved = both >> 16;
+  if (ctas > 1) {
+    if (tid == 0) S.count[1] = total;
+    cluster_sync_all();
+    for (int r = 0; r < rank; ++r) {
+      const uint32_t c = ld_cluster_u32(remote(&S.count[1], r));
+      gone += c & 0xffffu;
+      moved += c >> 16;
+    }
+  }
+  // The r-th hole is the r-th evicted slot: the evicted list says where it is until its mover has asked.
+  int32_t *ev = P.evicted_out + b * P.evicted_stride;
+  for (int i = i0; i < i1; ++i) {
+    const int slot = slot0 + i;
+    if (!stays(ev_keys[i], equal_rank)) {
+      if (slot < keep && KVD_BOUNDS_OK(static_cast<int>(gone) < len - keep, P.status)) ev[gone] = slot;
+      ev_keys[i] = EV_GONE | gone++;
+    } else {
+      ev_keys[i] = slot < keep ? static_cast<uint32_t>(slot) : EV_MOVES | moved++;
+    }
+  }
+  all_sync();
+  // Kept slots.  In place nothing is overwritten that is still to be read: weights come from `keep` and above or go back to
+  // where they are, the positions of the evicted are in shared memory.
+  int32_t *so = P.slots_out + b * P.cap_out;
+  for (int i = tid; i < n; i += EV_THREADS) {
+    const uint32_t what = ev_keys[i];
+    if (what & EV_GONE) continue;
+    int dst = static_cast<int>(what);
+    if (what & EV_MOVES) {
+      const int r = static_cast<int>(what & ~EV_MOVES);
+      if (!KVD_BOUNDS_OK(r < len - keep, P.status)) continue;
+      dst = __ldcg(ev + r);
+    }
+    if (!KVD_BOUNDS_OK(dst >= 0 && dst < keep, P.status)) continue;
+    so[dst] = slot0 + i;
+    if (P.positions_out) P.positions_out[b * P.cap_out + dst] = ev_pos[i];
+    if (P.weights_out) P.weights_out[b * P.cap_out + dst] = w[slot0 + i];
+  }
+  all_sync();
+  for (int i = tid; i < n; i += EV_THREADS) {
+    const uint32_t what = ev_keys[i];
+    if ((what & EV_GONE) && KVD_BOUNDS_OK(static_cast<int>(what & ~EV_GONE) < len - keep, P.status)) ev[what & ~EV_GONE] = ev_pos[i];
+  }
+}
+
+// Rows of the kept keys to their slots, K and V: four 16-byte pieces of each in flight per thread.  Bound by memory: every
+// kept row is read and written once (in place, only the movers').
+__global__ void __launch_bounds__(EV_ROW_THREADS) kvd_evict_rows_kernel(const __grid_constant__ EvictParams P, int tiles) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int b = static_cast<int>(blockIdx.x) / tiles, row0 = static_cast<int>(blockIdx.x) % tiles * P.rows_per_cta;
+  const int kept = min(P.keep, P.len[b]), rows = min(P.rows_per_cta, kept - row0);
+  if (rows <= 0) return;
+  const int32_t *so = P.slots_out + b * P.cap_out + row0;
+  const bool in_place = P.k == P.k_out;
+  const uint4 *src_of[2] = {P.k + b * P.cap_in * P.row_in, P.v + b * P.cap_in * P.row_in};
+  uint4 *dst_of[2] = {P.k_out + (b * P.cap_out + row0) * P.row_out, P.v_out + (b * P.cap_out + row0) * P.row_out};
+  const int pieces = rows * P.row_chunks;
+  for (int at = threadIdx.x; at < pieces; at += 4 * EV_ROW_THREADS) {
+    uint4 x[2][4];
+    long long to[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = at + u * EV_ROW_THREADS;
+      to[u] = -1;
+      if (i < pieces) {
+        const int r = i / P.row_chunks, c = i % P.row_chunks, slot = so[r];
+        if ((!in_place || slot != row0 + r) && KVD_BOUNDS_OK(slot >= 0 && slot < P.len[b], P.status)) {
+          to[u] = r * P.row_out + c;
+          x[0][u] = src_of[0][slot * P.row_in + c];
+          x[1][u] = src_of[1][slot * P.row_in + c];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (to[u] >= 0) {
+        dst_of[0][to[u]] = x[0][u];
+        dst_of[1][to[u]] = x[1][u];
+      }
+  }
+}
+
+}  // namespace kvd
+
+using namespace kvd;
+
+static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+extern "C" kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_cache *in, const int32_t *lens, int keep, int32_t protect_below,
+                                      const int32_t *protect_from, const kvd_ranked_cache *out, int32_t *slots_out, int32_t *evicted_out,
+                                      int64_t evicted_stride, void *stream_) {
+  if (!ctx || batch < 0 || keep < 0) return KVD_ERR_INVALID_ARG;
+  if (batch == 0) return KVD_OK;
+  if (!in || !out || !lens || !in->weights || !slots_out) return KVD_ERR_INVALID_ARG;
+  const kvd_model_desc &d = ctx->desc;
+  const int eb = ctx->dtype == KVD_DTYPE_F32 ? 4 : 2;
+  const int64_t kdim = static_cast<int64_t>(d.n_kv_heads) * d.d_head;
+  // rows are moved where there are rows: all four arrays, or none (the lists alone)
+  const bool rows = in->k != nullptr;
+  if ((in->v != nullptr) != rows || (out->k != nullptr) != rows || (out->v != nullptr) != rows) return KVD_ERR_INVALID_ARG;
+  if (in->slots < 0 || out->slots < 0 || (out->positions && !in->positions && in->slots > INT32_MAX)) return KVD_ERR_INVALID_ARG;
+  int max_len = 0, max_kept = 0, max_gone = 0;
+  for (int b = 0; b < batch; ++b) {
+    if (lens[b] < 0 || lens[b] > in->slots) return KVD_ERR_INVALID_ARG;
+    const int kept = lens[b] < keep ? lens[b] : keep;
+    max_len = lens[b] > max_len ? lens[b] : max_len;
+    max_kept = kept > max_kept ? kept : max_kept;
+    max_gone = lens[b] - kept > max_gone ? lens[b] - kept : max_gone;
+  }
+  if (max_len > KVD_MAX_EVICT_SLOTS || max_kept > out->slots || max_gone > evicted_stride) return KVD_ERR_CAPACITY;
+  if (max_gone > 0 && !evicted_out) return KVD_ERR_INVALID_ARG;
+  if (max_len == 0) return KVD_OK;
+  if (rows) {
+    if (in->row_stride < kdim || out->row_stride < kdim) return KVD_ERR_INVALID_ARG;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(in->k) | reinterpret_cast<uintptr_t>(in->v) | reinterpret_cast<uintptr_t>(out->k) | reinterpret_cast<uintptr_t>(out->v);
+    if ((p & 15u) != 0 || in->row_stride * eb % 16 != 0 || out->row_stride * eb % 16 != 0) return KVD_ERR_ALIGNMENT;
+    // in place: the same arrays with the same strides; otherwise nothing that is written may be read
+    const size_t nin = (static_cast<size_t>(batch - 1) * in->slots + max_len) * in->row_stride * eb, nout = (static_cast<size_t>(batch - 1) * out->slots + max_kept) * out->row_stride * eb;
+    const bool same = in->k == out->k && in->v == out->v && in->row_stride == out->row_stride && in->slots == out->slots;
+    if (!same && (overlap(in->k, nin, out->k, nout) || overlap(in->k, nin, out->v, nout) || overlap(in->v, nin, out->k, nout) || overlap(in->v, nin, out->v, nout)))
+      return KVD_ERR_INVALID_ARG;
+    if (overlap(out->k, nout, out->v, nout)) return KVD_ERR_INVALID_ARG;
+  }
+  const size_t win = (static_cast<size_t>(batch - 1) * in->slots + max_len) * 4, wout = (static_cast<size_t>(batch - 1) * out->slots + max_kept) * 4;
+  if (out->weights && !(out->weights == in->weights && out->slots == in->slots) && overlap(in->weights, win, out->weights, wout)) return KVD_ERR_INVALID_ARG;
+  if (out->positions && in->positions && !(out->positions == in->positions && out->slots == in->slots) && overlap(in->positions, win, out->positions, wout))
+    return KVD_ERR_INVALID_ARG;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+  // a cluster per sequence, of as many CTAs as its slots are worth
+  int ctas = 1;
+  while (ctas < EV_MAX_CTAS && max_len > ctas * EV_RUN) ctas *= 2;
+  static thread_local EvictParams P;
+  P.run = ((max_len + ctas - 1) / ctas + 3) / 4 * 4;
+  const size_t smem = sizeof(EvictShared) + static_cast<size_t>(P.run) * 8;
+  static std::atomic<bool> configured[64] = {};
+  cudaError_t e = opt_in_smem(ctx, kvd_evict_select_kernel, sizeof(EvictShared) + EV_CTA_SLOTS * 8, configured);
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "cudaFuncSetAttribute(evict)");
+  P.keep = keep;
+  P.protect_below = protect_below;
+  P.cap_in = in->slots;
+  P.cap_out = out->slots;
+  P.evicted_stride = evicted_stride;
+  P.row_in = rows ? in->row_stride * eb / 16 : 0;
+  P.row_out = rows ? out->row_stride * eb / 16 : 0;
+  P.row_chunks = static_cast<int>(kdim * eb / 16);
+  P.rows_per_cta = (4 * EV_ROW_THREADS + P.row_chunks - 1) / P.row_chunks;
+  P.status = ctx->d_status;
+  for (int b0 = 0; b0 < batch; b0 += EV_MAX_SEQS) {
+    const int nb = batch - b0 < EV_MAX_SEQS ? batch - b0 : EV_MAX_SEQS;
+    for (int i = 0; i < nb; ++i) {
+      P.len[i] = lens[b0 + i];
+      P.protect_from[i] = protect_from ? protect_from[b0 + i] : INT32_MAX;
+    }
+    P.weights = in->weights + static_cast<size_t>(b0) * in->slots;
+    P.positions = in->positions ? in->positions + static_cast<size_t>(b0) * in->slots : nullptr;
+    P.weights_out = out->weights ? out->weights + static_cast<size_t>(b0) * out->slots : nullptr;
+    P.positions_out = out->positions ? out->positions + static_cast<size_t>(b0) * out->slots : nullptr;
+    P.slots_out = slots_out + static_cast<size_t>(b0) * out->slots;
+    P.evicted_out = evicted_out ? evicted_out + static_cast<size_t>(b0) * evicted_stride : nullptr;
+    P.k = rows ? static_cast<const uint4 *>(in->k) + static_cast<size_t>(b0) * in->slots * P.row_in : nullptr;
+    P.v = rows ? static_cast<const uint4 *>(in->v) + static_cast<size_t>(b0) * in->slots * P.row_in : nullptr;
+    P.k_out = rows ? static_cast<uint4 *>(out->k) + static_cast<size_t>(b0) * out->slots * P.row_out : nullptr;
+    P.v_out = rows ? static_cast<uint4 *>(out->v) + static_cast<size_t>(b0) * out->slots * P.row_out : nullptr;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute attr[2];
+    cfg.stream = stream;
+    cfg.gridDim = dim3(nb * ctas, 1, 1);
+    cfg.blockDim = dim3(EV_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = (serial_launch_mask() & 8) || 2 * nb * ctas > ctx->num_sms ? 0 : 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kvd_evict_select_kernel, P, ctas);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "launch evict (select)");
+    ctx->launches += 1;
+    if (!rows || max_kept == 0) continue;
+    const int tiles = (max_kept + P.rows_per_cta - 1) / P.rows_per_cta;
+    cfg.gridDim = dim3(nb * tiles, 1, 1);
+    cfg.blockDim = dim3(EV_ROW_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = 0;
+    attr[0].val.programmaticStreamSerializationAllowed = serial_launch_mask() & 8 ? 0 : 1;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kvd_evict_rows_kernel, P, tiles);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "launch evict (rows)");
+    ctx->launches += 1;
+  }
+  return KVD_OK;
+}

@@ -8,6 +8,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <atomic>
 #include <map>
 #include <string>
 #include <vector>
@@ -203,6 +204,16 @@ struct AttnLaunchHead {
   int max_parts;           // slots the partial arrays hold
   bool early;              // both kernels start early whatever their grids
   bool tail;               // there is a sequence whose live keys the merge kernel attends itself (attn_tail)
+  float *scores;           // launches that weigh their keys: [n_seqs][n_q][score_stride], column 0 = chunk0_pos (log2 units)
+  long long score_stride;  // even
+};
+// ... and where the keys' weights go (n_positions per sequence; in may be null)
+struct AttnWeigh {
+  const float *in;
+  float *out;
+  long long stride;
+  int n_positions;
+  int tiles;  // CTAs per sequence
 };
 template <int NSEQ>
 struct AttnLaunchT : AttnLaunchHead {
@@ -365,6 +376,15 @@ inline cudaError_t launch_dependent(const kvd_ctx *ctx, void (*kern)(P...), dim3
   return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
 }
 
+// Shared memory above 48 KB is asked for once per kernel and device (`done`: a static of the caller's, one per kernel).
+template <typename F>
+inline cudaError_t opt_in_smem(const kvd_ctx *ctx, F *kern, size_t bytes, std::atomic<bool> (&done)[64]) {
+  if (done[ctx->device & 63].load(std::memory_order_acquire)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess) done[ctx->device & 63].store(true, std::memory_order_release);
+  return e;
+}
+
 // Schedule of a launch: its tiles (units of two, single ones, cut ones) and its CTA pairs.  The one place both the launch
 // and the size test of the trace buffer take the grid from.
 struct RcSchedule {
@@ -394,6 +414,7 @@ kvd_status launch_recompute_fused(kvd_ctx *ctx, const LayerState &ls, const CUte
 kvd_status prepare_rows_map(kvd_ctx *ctx, LayerState &ls, int k, int n_cols, bool heads);
 kvd_status launch_rows(kvd_ctx *ctx, const LayerState &ls, int k, RowsParams &p, bool heads, cudaStream_t stream);
 kvd_status launch_attention(kvd_ctx *ctx, const AttnLaunch &L, int d_head, int group, cudaStream_t stream);
+kvd_status launch_attention_weights(kvd_ctx *ctx, const AttnLaunch &L, int d_head, int group, const AttnWeigh &weigh, cudaStream_t stream);
 kvd_status launch_prepare_weights(kvd_ctx *ctx, const __nv_bfloat16 *w, const __nv_bfloat16 *gamma, __nv_bfloat16 *wt,
                                   int d_hidden, int n_cols, cudaStream_t stream);
 kvd_status launch_convert_gamma(kvd_ctx *ctx, const __nv_bfloat16 *g, float *out, int n, cudaStream_t stream);
@@ -412,6 +433,23 @@ kvd_status launch_checkpoint(kvd_ctx *ctx, const __nv_bfloat16 *rows, const int3
 kvd_status launch_selftest_bounds(kvd_ctx *ctx, cudaStream_t stream);
 kvd_status launch_checkpoint_scatter(kvd_ctx *ctx, const __nv_bfloat16 *rows, const int32_t *pos, const CkptSlots &slots,
                                      int n, int d_hidden, cudaStream_t stream);
+// kvd_shared_prefix_attention: the partials of a launch's sequences over the prefix they share
+struct SharedPrefixParams {
+  const __nv_bfloat16 *q;  // [sequences][n_q][d_head] (already offset to the launch's first sequence)
+  int n_q, n_kv;
+  float scale_log2e;
+  int rows, row_tiles;     // (sequence, head of the group) pairs of a KV head, tiles of 128 of them
+  int key0, n_blk, splits; // first key of the prefix that any sequence sees, blocks from there on, shares of them
+  float *part_o, *part_ml;
+  int max_parts;
+  int *status;
+  unsigned long long timeout_ns;
+  int lo[AT_MAX_SEQS], hi[AT_MAX_SEQS];  // first and last key of the prefix that a sequence sees (index into the segment)
+  int slot[AT_MAX_SEQS];                 // the sequence's first partial: one per split
+};
+int shared_prefix_block(int d_head);                         // keys per block
+int shared_prefix_tiles(int d_head, int row_tiles);          // row tiles per CTA
+kvd_status launch_shared_prefix(kvd_ctx *ctx, const SharedPrefixParams &P, const kvd_kv_segment &prefix, int d_head, int group, cudaStream_t stream);
 // kvd_prefill_attention: many query tokens of one sequence, tiled over query rows (Eq. 6-7 per row)
 struct PrefillParams {
   const __nv_bfloat16 *q;    // [n_rows][n_q][d_head]

@@ -180,6 +180,11 @@ __device__ __forceinline__ void tmem_alloc(uint32_t smem_result, uint32_t ncols)
 __device__ __forceinline__ void tmem_relinquish() {
   asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
 }
+// ... and let others allocate: for a kernel that takes what it needs once.
+__device__ __forceinline__ void tmem_claim(uint32_t smem_result, uint32_t ncols) {
+  tmem_alloc(smem_result, ncols);
+  tmem_relinquish();
+}
 __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }

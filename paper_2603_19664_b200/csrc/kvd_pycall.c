@@ -26,6 +26,14 @@ static kvd_status (*p_decode_step_kv)(kvd_ctx *, int, const kvd_store_range *, i
                                       void *, int64_t, void *);
 static kvd_status (*p_decode_attention)(kvd_ctx *, int, int, const void *, const int32_t *, const kvd_kv_segment *, int, float, void *, void *);
 static kvd_status (*p_prefill_attention)(kvd_ctx *, int, int, const void *, const int32_t *, const kvd_kv_segment *, int, float, void *, void *);
+static kvd_status (*p_shared_prefix_attention)(kvd_ctx *, int, int, const void *, const int32_t *, const kvd_kv_segment *, const kvd_kv_segment *, int, float,
+                                               void *, void *);
+static kvd_status (*p_decode_attention_weights)(kvd_ctx *, int, int, const void *, const int32_t *, const kvd_kv_segment *, int, float, void *, const float *,
+                                                float *, int64_t, int, void *, size_t, void *);
+static kvd_status (*p_prefill_attention_weights)(kvd_ctx *, int, int, const void *, const int32_t *, const kvd_kv_segment *, int, float, const float *, float *,
+                                                 int, void *, size_t, void *);
+static kvd_status (*p_cache_evict)(kvd_ctx *, int, const kvd_ranked_cache *, const int32_t *, int, int32_t, const int32_t *, const kvd_ranked_cache *, int32_t *,
+                                   int32_t *, int64_t, void *);
 
 static const struct {
   const char *name;
@@ -34,7 +42,9 @@ static const struct {
     {"kvd_reset_sequence", (void **)&p_reset_sequence},       {"kvd_checkpoint_residual", (void **)&p_checkpoint_residual},
     {"kvd_recompute_kv", (void **)&p_recompute_kv},           {"kvd_recompute_kv_step", (void **)&p_recompute_kv_step},
     {"kvd_decode_step_kv", (void **)&p_decode_step_kv},       {"kvd_decode_attention", (void **)&p_decode_attention},
-    {"kvd_prefill_attention", (void **)&p_prefill_attention},
+    {"kvd_prefill_attention", (void **)&p_prefill_attention}, {"kvd_shared_prefix_attention", (void **)&p_shared_prefix_attention},
+    {"kvd_decode_attention_weights", (void **)&p_decode_attention_weights},
+    {"kvd_prefill_attention_weights", (void **)&p_prefill_attention_weights}, {"kvd_cache_evict", (void **)&p_cache_evict},
 };
 
 static int as_i64(PyObject *o, int64_t *out) {
@@ -178,6 +188,33 @@ static int as_segments(PyObject *const *lists, Py_ssize_t rows, kvd_kv_segment *
   return 1;
 }
 
+/* the batch's lists of segments: 1, 0 (not of the plain kind), -1 (an exception is set) */
+static int as_segment_lists(PyObject *o, int batch, kvd_kv_segment *out, int *count) {
+  Py_ssize_t lists;
+  PyObject *held;
+  int ok;
+  if (items_of(o, &lists) == NULL || lists != batch) return 0;
+  held = PySequence_Tuple(o); /* (a copy of the outer list: the inner ones are held one by one) */
+  if (held == NULL) return -1;
+  ok = PyTuple_GET_SIZE(held) == batch && as_segments(PySequence_Fast_ITEMS(held), batch, out, count);
+  Py_DECREF(held);
+  return ok;
+}
+/* (k, v, positions, weights, row_stride, slots) */
+static int as_cache(PyObject *o, kvd_ranked_cache *c) {
+  Py_ssize_t n;
+  PyObject **it = PyTuple_CheckExact(o) ? items_of(o, &n) : NULL;
+  void *k, *v, *positions, *weights;
+  if (it == NULL || n != 6 || !as_tensor(it[0], &k, 1) || !as_tensor(it[1], &v, 1) || !as_tensor(it[2], &positions, 1) || !as_tensor(it[3], &weights, 1) ||
+      !as_i64(it[4], &c->row_stride) || !as_i64(it[5], &c->slots))
+    return 0;
+  c->k = k;
+  c->v = v;
+  c->positions = positions;
+  c->weights = weights;
+  return 1;
+}
+
 #define UNUSUAL return PyErr_Occurred() ? NULL : PyLong_FromLong(-1)
 #define CALL(expr)                    \
   do {                                \
@@ -246,24 +283,15 @@ static PyObject *py_decode_step_kv(PyObject *self, PyObject *const *a, Py_ssize_
 static PyObject *py_decode_attention(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   void *h, *q, *out, *stream;
   int layer, batch, n_segs;
-  Py_ssize_t lists;
-  PyObject **segs;
   int32_t pos[MAX_ENTRIES];
   kvd_kv_segment seg[MAX_ENTRIES];
   (void)self;
   if (n != 9 || !as_handle(a[0], &h) || !as_int(a[1], &layer) || !as_int(a[2], &batch) || batch < 1 || !as_tensor(a[3], &q, 1) ||
       !as_ints(a[4], batch, pos) || !PyFloat_CheckExact(a[6]) || !as_tensor(a[7], &out, 1) || !as_handle(a[8], &stream))
     UNUSUAL;
-  /* (a copy of the outer list: the inner ones are held one by one) */
-  segs = items_of(a[5], &lists);
-  if (segs == NULL || lists != batch) UNUSUAL;
-  {
-    PyObject *held = PySequence_Tuple(a[5]);
-    int ok;
-    if (held == NULL) return NULL;
-    ok = PyTuple_GET_SIZE(held) == batch && as_segments(PySequence_Fast_ITEMS(held), batch, seg, &n_segs);
-    Py_DECREF(held);
-    if (!ok) UNUSUAL;
+  switch (as_segment_lists(a[5], batch, seg, &n_segs)) {
+    case 0: UNUSUAL;
+    case -1: return NULL;
   }
   CALL(p_decode_attention(h, layer, batch, q, pos, seg, n_segs, (float)PyFloat_AS_DOUBLE(a[6]), out, stream));
 }
@@ -277,6 +305,70 @@ static PyObject *py_prefill_attention(PyObject *self, PyObject *const *a, Py_ssi
       !as_segments(&a[5], 1, seg, &n_segs) || !PyFloat_CheckExact(a[6]) || !as_tensor(a[7], &out, 1) || !as_handle(a[8], &stream))
     UNUSUAL;
   CALL(p_prefill_attention(h, layer, rows, q, pos, seg, n_segs, (float)PyFloat_AS_DOUBLE(a[6]), out, stream));
+}
+
+/* (ctx, layer, batch, q, q_pos, prefix, segs, scale, out, stream) */
+static PyObject *py_shared_prefix_attention(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  void *h, *q, *out, *stream;
+  int layer, batch, n_segs;
+  int32_t pos[MAX_ENTRIES];
+  kvd_kv_segment prefix, seg[MAX_ENTRIES];
+  (void)self;
+  if (n != 10 || !as_handle(a[0], &h) || !as_int(a[1], &layer) || !as_int(a[2], &batch) || batch < 1 || !as_tensor(a[3], &q, 1) ||
+      !as_ints(a[4], batch, pos) || !as_segment(a[5], &prefix) || !PyFloat_CheckExact(a[7]) || !as_tensor(a[8], &out, 1) || !as_handle(a[9], &stream))
+    UNUSUAL;
+  switch (as_segment_lists(a[6], batch, seg, &n_segs)) {
+    case 0: UNUSUAL;
+    case -1: return NULL;
+  }
+  CALL(p_shared_prefix_attention(h, layer, batch, q, pos, &prefix, seg, n_segs, (float)PyFloat_AS_DOUBLE(a[7]), out, stream));
+}
+/* (ctx, layer, batch, q, q_pos, segs, scale, out, weights_in, weights_out, weights_stride, n_positions, scratch, scratch_bytes, stream) */
+static PyObject *py_decode_attention_weights(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  void *h, *q, *out, *in, *weights, *scratch, *stream;
+  int layer, batch, n_segs, positions;
+  int64_t stride, size;
+  int32_t pos[MAX_ENTRIES];
+  kvd_kv_segment seg[MAX_ENTRIES];
+  (void)self;
+  if (n != 15 || !as_handle(a[0], &h) || !as_int(a[1], &layer) || !as_int(a[2], &batch) || batch < 1 || !as_tensor(a[3], &q, 1) ||
+      !as_ints(a[4], batch, pos) || !PyFloat_CheckExact(a[6]) || !as_tensor(a[7], &out, 1) || !as_tensor(a[8], &in, 1) || !as_tensor(a[9], &weights, 1) ||
+      !as_i64(a[10], &stride) || !as_int(a[11], &positions) || !as_tensor(a[12], &scratch, 1) || !as_i64(a[13], &size) || size < 0 ||
+      !as_handle(a[14], &stream))
+    UNUSUAL;
+  switch (as_segment_lists(a[5], batch, seg, &n_segs)) {
+    case 0: UNUSUAL;
+    case -1: return NULL;
+  }
+  CALL(p_decode_attention_weights(h, layer, batch, q, pos, seg, n_segs, (float)PyFloat_AS_DOUBLE(a[6]), out, in, weights, stride, positions, scratch,
+                                  (size_t)size, stream));
+}
+/* (ctx, layer, n_rows, q, q_pos, segs, scale, weights_in, weights_out, n_positions, scratch, scratch_bytes, stream) */
+static PyObject *py_prefill_attention_weights(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  void *h, *q, *pos, *in, *weights, *scratch, *stream;
+  int layer, rows, n_segs, positions;
+  int64_t size;
+  kvd_kv_segment seg[MAX_ENTRIES];
+  (void)self;
+  if (n != 13 || !as_handle(a[0], &h) || !as_int(a[1], &layer) || !as_int(a[2], &rows) || !as_tensor(a[3], &q, 1) || !as_tensor(a[4], &pos, 1) ||
+      !as_segments(&a[5], 1, seg, &n_segs) || !PyFloat_CheckExact(a[6]) || !as_tensor(a[7], &in, 1) || !as_tensor(a[8], &weights, 1) ||
+      !as_int(a[9], &positions) || !as_tensor(a[10], &scratch, 1) || !as_i64(a[11], &size) || size < 0 || !as_handle(a[12], &stream))
+    UNUSUAL;
+  CALL(p_prefill_attention_weights(h, layer, rows, q, pos, seg, n_segs, (float)PyFloat_AS_DOUBLE(a[6]), in, weights, positions, scratch, (size_t)size, stream));
+}
+/* (ctx, batch, cache, lens, keep, protect_below, protect_from, cache_out, slots_out, evicted_out, evicted_stride, stream) */
+static PyObject *py_cache_evict(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  void *h, *slots, *evicted, *stream;
+  int batch, keep, below;
+  int64_t stride;
+  int32_t lens[MAX_ENTRIES], from[MAX_ENTRIES];
+  kvd_ranked_cache in, out;
+  (void)self;
+  if (n != 12 || !as_handle(a[0], &h) || !as_int(a[1], &batch) || batch < 1 || !as_cache(a[2], &in) || !as_ints(a[3], batch, lens) || !as_int(a[4], &keep) ||
+      !as_int(a[5], &below) || (a[6] != Py_None && !as_ints(a[6], batch, from)) || !as_cache(a[7], &out) || !as_tensor(a[8], &slots, 1) ||
+      !as_tensor(a[9], &evicted, 1) || !as_i64(a[10], &stride) || !as_handle(a[11], &stream))
+    UNUSUAL;
+  CALL(p_cache_evict(h, batch, &in, lens, keep, below, a[6] == Py_None ? NULL : from, &out, slots, evicted, stride, stream));
 }
 
 /* bind(name, address): the library's entry point of that name */
@@ -300,7 +392,9 @@ static PyObject *py_bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
 
 #define FAST(name) {"kvd_" #name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef k_methods[] = {FAST(reset_sequence),   FAST(checkpoint_residual), FAST(recompute_kv),      FAST(recompute_kv_step),
-                                  FAST(decode_step_kv),   FAST(decode_attention),    FAST(prefill_attention), {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, NULL},
+                                  FAST(decode_step_kv),   FAST(decode_attention),    FAST(prefill_attention),
+                                  FAST(shared_prefix_attention), FAST(decode_attention_weights), FAST(prefill_attention_weights), FAST(cache_evict),
+                                  {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, NULL},
                                   {NULL, NULL, 0, NULL}};
 static struct PyModuleDef k_module = {PyModuleDef_HEAD_INIT, "_kvdcall", NULL, -1, k_methods, NULL, NULL, NULL, NULL};
 
