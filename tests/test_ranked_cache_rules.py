@@ -16,7 +16,7 @@ for _f in ("kvd_prefill_weights.cu", "kvd_shared_prefix.cu", "kvd_evict.cu", "kv
             depth += {"{": 1, "}": -1}.get(_text[i], 0)
             i += 1
         KERNELS[_m.group(1)] = (_m.group(2), _text[_m.end():i])
-NEW = ["kvd_prefill_weights_kernel", "kvd_prefill_weights_rows_kernel", "kvd_prefill_weights_sum_kernel", "kvd_shared_prefix_kernel", "kvd_evict_select_kernel",
+NEW = ["kvd_prefill_weights_kernel", "kvd_prefill_weights_sum_kernel", "kvd_shared_prefix_kernel", "kvd_evict_select_kernel",
        "kvd_evict_rows_kernel", "kvd_attn_merge_weigh_kernel"]
 
 
@@ -34,7 +34,14 @@ def test_dependents_start_only_after_tensor_memory_is_allocated(name):
     claim, start = body.index("tmem_claim"), body.index("grid_launch_dependents")
     assert claim < start and "__syncthreads()" in body[claim:start]
     # ... and is given back behind a barrier that every role reaches, whatever ran out of time
-    assert "return" not in re.sub(r"\[&\][^{]*\{[^{}]*\}", "", body[start:body.index("tmem_dealloc")])
+    rest = body[start:body.index("tmem_dealloc")]
+    for m in reversed(list(re.finditer(r"\[&\]\([^)]*\) \{", rest))):  # (what lambdas return)
+        depth, i = 1, m.end()
+        while depth:
+            depth += {"{": 1, "}": -1}.get(rest[i], 0)
+            i += 1
+        rest = rest[:m.start()] + rest[i:]
+    assert "return" not in rest
 
 
 def test_every_wait_has_a_limit():
