@@ -863,7 +863,23 @@ __device__ __forceinline__ void attn_weigh_cta(const AttnLaunchT<NSEQ> &P, const
   const int si = block / W.tiles, pos0 = block % W.tiles * (2 * static_cast<int>(blockDim.x)), p = pos0 + 2 * static_cast<int>(threadIdx.x);
   const AttnSeq &S = P.seq[si];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = static_cast<int>(blockDim.x) >> 5;
-  const bool some = S.n_chunks > 0 && pos0 <= S.hi_pos && ends_by(pos0, 2 * static_cast<int>(blockDim.x), S.lo_pos - 1) == false;
+  const bool some = S.n_chunks > 0 && pos0 <= S.hi_pos && !ends_by(pos0, 2 * static_cast<int>(blockDim.x), S.lo_pos - 1);
+  // which of the two keys the query sees, and the first heads' scores of both, on their way while the statistics are made
+  constexpr int AHEAD = 8;
+  bool see0 = false, see1 = false;
+  float2 first[AHEAD];
+  const float *sc = P.scores + static_cast<size_t>(si) * P.n_q * P.score_stride + (p - S.chunk0_pos);
+  if (some && p < W.n_positions) {
+#pragma unroll
+    for (int sg = 0; sg < KVD_MAX_SEGMENTS; ++sg) {
+      see0 |= p >= S.lo_pos && p <= S.hi_pos && segment_holds(S.first[sg], S.len[sg], p, 1);
+      see1 |= p + 1 >= S.lo_pos && p < S.hi_pos && segment_holds(S.first[sg], S.len[sg], p + 1, 1);
+    }
+  }
+  const bool see = see0 || see1;
+#pragma unroll
+  for (int h = 0; h < AHEAD; ++h)
+    first[h] = see && h < P.n_q ? __ldcg(reinterpret_cast<const float2 *>(sc + static_cast<size_t>(h) * P.score_stride)) : make_float2(-CUDART_INF_F, -CUDART_INF_F);
   const int count = KVD_BOUNDS_OK(S.slot_base >= 0 && S.slot_base + S.n_chunks <= P.max_parts, P.status) ? S.n_chunks : 0;
   if (some) {
     const float2 *ml0 = reinterpret_cast<const float2 *>(P.part_ml) + static_cast<size_t>(S.merge_base) * P.n_q;
@@ -893,26 +909,25 @@ __device__ __forceinline__ void attn_weigh_cta(const AttnLaunchT<NSEQ> &P, const
   __syncthreads();
   if (p >= W.n_positions) return;
   float w0 = 0.f, w1 = 0.f;
-  if (some) {
-    const bool in0 = p >= S.lo_pos && p <= S.hi_pos, in1 = p + 1 >= S.lo_pos && p < S.hi_pos;
-    bool see0 = false, see1 = false;
+  if (see) {
+    auto add = [&](int h, float2 s) {
+      const float nl = at_merge_smem[h];
+      w0 += exp2f(s.x + nl);
+      w1 += exp2f(s.y + nl);
+    };
+    for (int h0 = 0; h0 < P.n_q; h0 += AHEAD) {
+      float2 now[AHEAD];
 #pragma unroll
-    for (int sg = 0; sg < KVD_MAX_SEGMENTS; ++sg) {
-      see0 |= in0 && segment_holds(S.first[sg], S.len[sg], p, 1);
-      see1 |= in1 && segment_holds(S.first[sg], S.len[sg], p + 1, 1);
-    }
-    if (see0 || see1) {
-      const float *sc = P.scores + static_cast<size_t>(si) * P.n_q * P.score_stride + (p - S.chunk0_pos);
-#pragma unroll 8
-      for (int h = 0; h < P.n_q; ++h) {
-        const float2 s = __ldcg(reinterpret_cast<const float2 *>(sc + static_cast<size_t>(h) * P.score_stride));
-        const float nl = at_merge_smem[h];
-        w0 += exp2f(s.x + nl);
-        w1 += exp2f(s.y + nl);
+      for (int h = 0; h < AHEAD; ++h) {
+        now[h] = first[h];
+        if (h0 + AHEAD + h < P.n_q) first[h] = __ldcg(reinterpret_cast<const float2 *>(sc + static_cast<size_t>(h0 + AHEAD + h) * P.score_stride));
       }
-      if (!see0) w0 = 0.f;
-      if (!see1) w1 = 0.f;
+#pragma unroll
+      for (int h = 0; h < AHEAD; ++h)
+        if (h0 + h < P.n_q) add(h0 + h, now[h]);
     }
+    if (!see0) w0 = 0.f;
+    if (!see1) w1 = 0.f;
   }
   const size_t at = static_cast<size_t>(si) * W.stride + p;
   W.out[at] = (W.in ? W.in[at] : 0.f) + w0;
@@ -1019,6 +1034,8 @@ static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t str
     const int warps = (groups < most ? groups : most) + own;
     merge_warps = warps > merge_warps ? warps : merge_warps;
   }
+  // (a CTA of the weights puts the heads' statistics together, a head per warp and turn: nine heads of 100 keys 9.4 us with one warp)
+  if (WEIGH && merge_warps < 8) merge_warps = 8;
   // (the heads the fused recompute exists for)
   constexpr bool TAILS = (D_HEAD == 256 && G <= 2) || (D_HEAD == 128 && (G <= 2 || G == 4));
   cfg.blockDim = dim3(32 * merge_warps, 1, 1);

@@ -25,9 +25,10 @@ namespace kvd {
 constexpr int EV_THREADS = 1024;
 constexpr int EV_WARPS = EV_THREADS / 32;
 constexpr int EV_BINS = 2048;
+constexpr int EV_BATCH = 8;                       // slots whose loads a thread has in flight
 constexpr int EV_MAX_CTAS = 8;                    // a portable cluster
 constexpr int EV_CTA_SLOTS = KVD_MAX_EVICT_SLOTS / EV_MAX_CTAS;
-constexpr int EV_RUN = 1024;                      // slots that one CTA is enough for
+constexpr int EV_RUN = 8192;                      // slots that one CTA is enough for
 constexpr uint32_t EV_PROTECTED = 0xffffffffu;    // above the key of plus infinity, 0xff800000
 constexpr uint32_t EV_GONE = 0x80000000u, EV_MOVES = 0x40000000u;
 constexpr int EV_MAX_SEQS = 64;
@@ -49,11 +50,12 @@ struct EvictParams {
   int len[EV_MAX_SEQS], protect_from[EV_MAX_SEQS];
 };
 
+static_assert(6 * EV_BINS >= EV_RUN, "a single CTA's holes");
 struct EvictShared {
-  uint32_t hist[3][EV_BINS];    // this CTA's counts, by pass
+  uint32_t hist[3][EV_BINS];    // this CTA's counts, by pass; a single CTA's holes after that
   uint32_t sum[3][EV_BINS];     // rank 0: the cluster's, added up by remote atomics
   uint32_t warp_sum[EV_WARPS], part[2][EV_WARPS];
-  uint32_t digit, above;        // found in the current pass
+  uint32_t digit, above, through;  // found in the current pass: the digit, counts of the keys above it, and with it
   uint32_t count[2];            // of this CTA's run: slots equal to T; evicted ones and movers
 };
 
@@ -100,12 +102,25 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
   const int from = P.protect_from[b];
   auto is_protected = [&](int p) { return p < P.protect_below || p >= from; };
   all_sync();  // histograms are clear everywhere
-  for (int i = tid; i < n; i += EV_THREADS) {
-    const int p = pos ? pos[slot0 + i] : slot0 + i;
-    const uint32_t key = is_protected(p) ? EV_PROTECTED : evict_key(w[slot0 + i]);
-    ev_keys[i] = key;
-    ev_pos[i] = p;
-    if (keep < len) atomicAdd(&S.hist[0][key >> 21], 1u);
+  for (int at = tid; at < n; at += EV_BATCH * EV_THREADS) {
+    int p[EV_BATCH];
+    float x[EV_BATCH];
+#pragma unroll
+    for (int u = 0; u < EV_BATCH; ++u) {
+      const int i = at + u * EV_THREADS;
+      p[u] = i < n && pos ? pos[slot0 + i] : slot0 + i;
+      x[u] = i < n ? w[slot0 + i] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < EV_BATCH; ++u) {
+      const int i = at + u * EV_THREADS;
+      if (i < n) {
+        const uint32_t key = is_protected(p[u]) ? EV_PROTECTED : evict_key(x[u]);
+        ev_keys[i] = key;
+        ev_pos[i] = p[u];
+        if (keep < len) atomicAdd(&S.hist[0][key >> 21], 1u);
+      }
+    }
   }
   // ---- T: the keep-th largest key; need: how many of the slots equal to it stay
   uint32_t T, need;
@@ -151,12 +166,18 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
       if (a0 < need && need <= a1) {
         S.digit = EV_BINS - 1 - 2 * tid;
         S.above = a0;
+        S.through = a1;
       } else if (a1 < need && need <= a2) {
         S.digit = EV_BINS - 2 - 2 * tid;
         S.above = a1;
+        S.through = a2;
       }
       __syncthreads();
       T |= S.digit << shift;
+      if (S.through == need) {  // all keys that agree with T so far stay: none of them is below it
+        need = 0x7fffffffu;
+        break;
+      }
       need -= S.above;
       if (pass < 2) {
         const int next = pass == 0 ? 10 : 0;
@@ -186,40 +207,57 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
     }
   }
   __syncthreads();
-  // ---- ranks.  Thread t owns the slots [t * per, (t + 1) * per) of the run, so that prefix counts over threads are in slot
-  // order.  A slot's key gives way to what becomes of it: its own index (stays), EV_MOVES | rank, EV_GONE | rank.
-  const int per = (n + EV_THREADS - 1) / EV_THREADS;
-  const int i0 = min(n, tid * per), i1 = min(n, i0 + per);
-  auto block_excl = [&](uint32_t mine, uint32_t (&warp_part)[EV_WARPS], uint32_t *total) {  // counts of the threads before this one
+  // ---- ranks.  A warp owns a contiguous part of the run, 32 slots to a turn, and lane t keeps what concerns turn t as masks:
+  // counts of lanes, turns, warps and CTAs before a slot are then counts in slot order.  A slot's key gives way to what becomes
+  // of it: its own index (stays), EV_MOVES | rank, EV_GONE | rank.
+  const int turns = (n + EV_THREADS - 1) / EV_THREADS, i0 = min(n, warp * turns * 32), i1 = min(n, i0 + turns * 32);
+  const uint32_t before_me = (1u << lane) - 1u;
+  auto lower = [](int k) { return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1u; };
+  auto lanes_before = [&](uint32_t mine, uint32_t *total) {
     uint32_t incl = mine;
 #pragma unroll
     for (int k = 1; k < 32; k <<= 1) {
       const uint32_t o = __shfl_up_sync(0xffffffffu, incl, k);
       if (lane >= k) incl += o;
     }
-    if (lane == 31) warp_part[warp] = incl;
-    __syncthreads();
-    const uint32_t v = warp_part[lane];
-    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u);
-    *total = __reduce_add_sync(0xffffffffu, v);
-    return before + incl - mine;
+    *total = __shfl_sync(0xffffffffu, incl, 31);
+    return incl - mine;
   };
-  // above T, or one of the lowest `need` equal to it (rank: of those before it)
-  auto stays = [&](uint32_t key, uint32_t &rank_of_equal) { return keep == len || (keep > 0 && (key > T || (key == T && rank_of_equal++ < need))); };
-  uint32_t equal = 0, total;
-  for (int i = i0; i < i1; ++i) equal += ev_keys[i] == T;
-  uint32_t equal_rank = block_excl(equal, S.part[0], &total);
+  auto warps_before = [&](uint32_t mine, uint32_t (&of_warp)[EV_WARPS], uint32_t *total) {  // (mine: the same in all lanes)
+    if (lane == 0) of_warp[warp] = mine;
+    __syncthreads();
+    const uint32_t v = of_warp[lane];
+    *total = __reduce_add_sync(0xffffffffu, v);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u);
+  };
+  uint32_t same = 0, stay = 0, total, of_warp;  // of turn `lane`: slots whose key is T, and those above
+#pragma unroll 4
+  for (int t = 0; t < turns; ++t) {
+    const int i = i0 + 32 * t + lane;
+    const uint32_t key = i < i1 ? ev_keys[i] : 0u;
+    const uint32_t eq = __ballot_sync(0xffffffffu, i < i1 && key == T), gt = __ballot_sync(0xffffffffu, i < i1 && key > T);
+    if (lane == t) {
+      same = eq;
+      stay = gt;
+    }
+  }
+  const int base = i0 + 32 * lane;
+  const uint32_t there = lane < turns ? lower(i1 - base) : 0u, high = ~lower(keep - slot0 - base);
+  uint32_t equal = lanes_before(__popc(same), &of_warp);
+  equal += warps_before(of_warp, S.part[0], &total);
   if (ctas > 1) {
     if (tid == 0) S.count[0] = total;
     cluster_sync_all();
-    for (int r = 0; r < rank; ++r) equal_rank += ld_cluster_u32(remote(&S.count[0], r));
+    for (int r = 0; r < rank; ++r) equal += ld_cluster_u32(remote(&S.count[0], r));
   }
-  uint32_t both = 0;  // evicted slots, and movers in the upper half (a run has fewer than 2^16 slots)
-  {
-    uint32_t er = equal_rank;
-    for (int i = i0; i < i1; ++i) both += !stays(ev_keys[i], er) ? 1u : slot0 + i >= keep ? 0x10000u : 0u;
-  }
-  both = block_excl(both, S.part[1], &total);
+  // of those equal to T the lowest `need` of the sequence
+  if (keep == len) stay = there;
+  else if (keep == 0) stay = 0u;
+  else if (equal + __popc(same) <= need) stay |= same;
+  else if (equal < need) stay |= same & lower(static_cast<int>(__fns(same, 0, static_cast<int>(need - equal) + 1)));
+  // evicted slots, and movers in the upper half (a run has fewer than 2^16 slots)
+  uint32_t both = lanes_before(__popc(there & ~stay) + (__popc(stay & high) << 16), &of_warp);
+  both += warps_before(of_warp, S.part[1], &total);
   uint32_t gone = both & 0xffffu, moved = both >> 16;
   if (ctas > 1) {
     if (tid == 0) S.count[1] = total;
@@ -230,36 +268,60 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
       moved += c >> 16;
     }
   }
-  // The r-th hole is the r-th evicted slot: the evicted list says where it is until its mover has asked.
+  // The r-th hole is the r-th evicted slot.  Its mover learns of it from shared memory (where the counts were), in a cluster from
+  // the evicted list, which gets its positions once all have asked.
+  uint32_t *holes = &S.hist[0][0];
   int32_t *ev = P.evicted_out + b * P.evicted_stride;
-  for (int i = i0; i < i1; ++i) {
-    const int slot = slot0 + i;
-    if (!stays(ev_keys[i], equal_rank)) {
-      if (slot < keep && KVD_BOUNDS_OK(static_cast<int>(gone) < len - keep, P.status)) ev[gone] = slot;
-      ev_keys[i] = EV_GONE | gone++;
-    } else {
-      ev_keys[i] = slot < keep ? static_cast<uint32_t>(slot) : EV_MOVES | moved++;
+#pragma unroll 4
+  for (int t = 0; t < turns; ++t) {
+    const int i = i0 + 32 * t + lane, slot = slot0 + i;
+    const uint32_t stay_t = __shfl_sync(0xffffffffu, stay, t), there_t = __shfl_sync(0xffffffffu, there, t), high_t = __shfl_sync(0xffffffffu, high, t);
+    const uint32_t gone_t = __shfl_sync(0xffffffffu, gone, t), moved_t = __shfl_sync(0xffffffffu, moved, t);
+    if (i < i1) {
+      if ((stay_t >> lane) & 1u) {
+        ev_keys[i] = slot < keep ? static_cast<uint32_t>(slot) : EV_MOVES | (moved_t + __popc(stay_t & high_t & before_me));
+      } else {
+        const uint32_t r = gone_t + __popc(there_t & ~stay_t & before_me);
+        if (slot < keep && KVD_BOUNDS_OK(static_cast<int>(r) < len - keep, P.status)) {
+          if (ctas > 1) ev[r] = slot;
+          else holes[r] = static_cast<uint32_t>(slot);
+        }
+        ev_keys[i] = EV_GONE | r;
+      }
     }
   }
   all_sync();
   // Kept slots.  In place nothing is overwritten that is still to be read: weights come from `keep` and above or go back to
   // where they are, the positions of the evicted are in shared memory.
   int32_t *so = P.slots_out + b * P.cap_out;
-  for (int i = tid; i < n; i += EV_THREADS) {
-    const uint32_t what = ev_keys[i];
-    if (what & EV_GONE) continue;
-    int dst = static_cast<int>(what);
-    if (what & EV_MOVES) {
-      const int r = static_cast<int>(what & ~EV_MOVES);
-      if (!KVD_BOUNDS_OK(r < len - keep, P.status)) continue;
-      dst = __ldcg(ev + r);
+  for (int at = tid; at < n; at += EV_BATCH * EV_THREADS) {
+    int dst[EV_BATCH];
+    float x[EV_BATCH];
+#pragma unroll
+    for (int u = 0; u < EV_BATCH; ++u) {
+      const int i = at + u * EV_THREADS;
+      const uint32_t what = i < n ? ev_keys[i] : EV_GONE;
+      const int r = static_cast<int>(what & ~(EV_MOVES | EV_GONE));
+      dst[u] = static_cast<int>(what);  // (negative: gone)
+      if ((what & (EV_GONE | EV_MOVES)) == EV_MOVES) dst[u] = !KVD_BOUNDS_OK(r < len - keep, P.status) ? keep : ctas > 1 ? __ldcg(ev + r) : static_cast<int>(holes[r]);
+      if (i >= n) dst[u] = keep;
+      x[u] = dst[u] >= 0 && i < n && P.weights_out ? w[slot0 + i] : 0.f;
     }
-    if (!KVD_BOUNDS_OK(dst >= 0 && dst < keep, P.status)) continue;
-    so[dst] = slot0 + i;
-    if (P.positions_out) P.positions_out[b * P.cap_out + dst] = ev_pos[i];
-    if (P.weights_out) P.weights_out[b * P.cap_out + dst] = w[slot0 + i];
+#pragma unroll
+    for (int u = 0; u < EV_BATCH; ++u) {
+      const int i = at + u * EV_THREADS;
+      if (dst[u] < 0) {
+        if (ctas == 1 && KVD_BOUNDS_OK((dst[u] & 0x7fffffff) < len - keep, P.status)) ev[dst[u] & 0x7fffffff] = ev_pos[i];
+      } else if (dst[u] < keep) {
+        so[dst[u]] = slot0 + i;
+        if (P.positions_out) P.positions_out[b * P.cap_out + dst[u]] = ev_pos[i];
+        if (P.weights_out) P.weights_out[b * P.cap_out + dst[u]] = x[u];
+      }
+    }
   }
-  all_sync();
+  if (ctas == 1) return;
+  cluster_sync_all();
+#pragma unroll 4
   for (int i = tid; i < n; i += EV_THREADS) {
     const uint32_t what = ev_keys[i];
     if ((what & EV_GONE) && KVD_BOUNDS_OK(static_cast<int>(what & ~EV_GONE) < len - keep, P.status)) ev[what & ~EV_GONE] = ev_pos[i];
