@@ -972,6 +972,7 @@ static kvd_status build_attn_launch(kvd_ctx *ctx, const LayerState &ls, int b0, 
   // (counted as if all live keys were streamed: what is refused does not hang on which kernel takes them)
   if (streamed_slots > ctx->max_parts) return KVD_ERR_CAPACITY;
   const float sc = scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(d.d_head));
+  L.beside = false;
   L.n_seqs = nb;
   L.total_chunks = parts;
   L.n_q = d.n_q_heads;
@@ -1066,8 +1067,8 @@ extern "C" kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int b
       int pre[AT_MAX_SEQS];
       P.splits = 0;
       if (hi_all >= 0) {
-        P.rows = nb * group;
-        P.row_tiles = (P.rows + 127) / 128;
+        P.seqs = nb;
+        P.row_tiles = (nb + 128 / group - 1) / (128 / group);
         P.key0 = lo_all;
         const int bk = shared_prefix_block(d.d_head), nt = shared_prefix_tiles(d.d_head, P.row_tiles);
         P.n_blk = (hi_all - lo_all) / bk + 1;
@@ -1100,6 +1101,7 @@ extern "C" kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int b
         st = launch_shared_prefix(ctx, P, *prefix, d.d_head, group, stream);
         if (st != KVD_OK) return st;
       }
+      L.beside = P.splits > 0;
       st = launch_attention(ctx, L, d.d_head, group, stream);
       if (st != KVD_OK) return st;
     }

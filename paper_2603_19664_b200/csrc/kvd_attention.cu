@@ -69,6 +69,12 @@ __device__ __forceinline__ float reduce8_transposed(const float (&v)[8], int lig
   return w1;
 }
 
+// End of a CTA of the streaming kernels.  One that ran beside the shared prefix's kernel: the grid is complete only when that kernel
+// is, too, so that whatever follows waits for both.
+__device__ __forceinline__ void finish_beside(bool beside) {
+  if (beside && blockIdx.x + 1 == gridDim.x) grid_dependency_wait();
+}
+
 // Where the keys of one warp iteration (a run of n <= 32) lie.  A chunk inside one segment and inside the visible range
 // (the common case) has addresses linear in the position; of any other chunk each run is asked for by itself, and only a
 // run that crosses an edge is looked up key by key, one key per lane.  The choice is uniform over the warp and does not
@@ -158,8 +164,9 @@ __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_at
   const int chunk_keys = KPL * U * AT_WARPS * S.iters;
   const int chunk_pos0 = S.chunk0_pos + chunk * chunk_keys;
 
-  // everything above used kernel parameters only; K, V and q may come from the preceding kernel
-  grid_dependency_wait();
+  // everything above used kernel parameters only; K, V and q may come from the preceding kernel.  (Beside the shared prefix's
+  // kernel, which lets its dependents in when everything ahead of it is complete, there is nothing to wait for.)
+  if (!P.beside) grid_dependency_wait();
   // ---- query of every head of the group, pre-multiplied by scale * log2(e)
   uint64_t qf[G][4];  // channel pairs (2j, 2j+1)
   auto load_query = [&]() {
@@ -367,6 +374,7 @@ __global__ void __launch_bounds__(AT_THREADS, ALLIN ? 2 : AT_CTAS_PER_SM) kvd_at
       P.part_ml[hq * 2 + 1] = l;
     }
   }
+  finish_beside(P.beside);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -455,7 +463,7 @@ __global__ void __launch_bounds__(AT_THREADS, SLOTS == 3 ? AT_CTAS_PER_SM : 3)
   const size_t head_el = static_cast<size_t>(kvh) * D_HEAD;
   const KeyRun whole = key_run(S, chunk_pos0, chunk_keys, head_el);
 
-  grid_dependency_wait();
+  if (!P.beside) grid_dependency_wait();
   // ---- pieces come in by whole rows (lane group grp's LPK lanes fetch row KPL u + grp) and are read as fragments: chunk c
   // (16 bytes) of row r of a piece of keys lies at c ^ 4 (r & 1), of values at c ^ 2 (r / 2 & 3), so that the eight lanes
   // that a shared-memory access serves at a time meet different banks (rows g8 of keys, rows 2 t and 2 t + 1 of values)
@@ -642,6 +650,7 @@ __global__ void __launch_bounds__(AT_THREADS, SLOTS == 3 ? AT_CTAS_PER_SM : 3)
       P.part_ml[hq * 2 + 1] = l;
     }
   }
+  finish_beside(P.beside);
 }
 
 // Second kernel of a decode step: the chunk partials of every (sequence, KV head) are merged in chunk
@@ -1004,6 +1013,7 @@ static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t str
   const bool small = S.total_chunks * S.n_kv <= num_sms * AT_CTAS_PER_SM;
   if (S.total_chunks > 0) {
     attr[0].val.programmaticStreamSerializationAllowed = ((small || S.early) && !(serial_launch_mask() & 2)) ? 1 : 0;
+    if (S.beside) attr[0].val.programmaticStreamSerializationAllowed = serial_launch_mask() & 2 ? 0 : 1;
     cfg.gridDim = dim3(S.total_chunks * S.n_kv, 1, 1);
     cfg.blockDim = dim3(AT_THREADS, 1, 1);
     if constexpr (G >= 3 && D_HEAD <= 128) {
@@ -1298,7 +1308,7 @@ extern "C" kvd_status kvd_decode_attention_static(int n_q_heads, int n_kv_heads,
   L.part_o = reinterpret_cast<float *>(scratch + ml_bytes);
   L.status = nullptr;
   L.max_parts = parts;
-  L.early = L.tail = false;
+  L.early = L.tail = L.beside = false;
   switch (d_head) {
     case 64: return static_launch_d<64>(L, group, stream);
     case 128: return static_launch_d<128>(L, group, stream);

@@ -203,6 +203,7 @@ struct AttnLaunchHead {
   int *status;             // device status word (nullptr: none), used by the checking build
   int max_parts;           // slots the partial arrays hold
   bool early;              // both kernels start early whatever their grids
+  bool beside;             // behind the shared prefix's kernel: the streaming kernel starts beside it, the merge waits for both
   bool tail;               // there is a sequence whose live keys the merge kernel attends itself (attn_tail)
   float *scores;           // launches that weigh their keys: [n_seqs][n_q][score_stride], column 0 = chunk0_pos (log2 units)
   long long score_stride;  // even
@@ -438,7 +439,7 @@ struct SharedPrefixParams {
   const __nv_bfloat16 *q;  // [sequences][n_q][d_head] (already offset to the launch's first sequence)
   int n_q, n_kv;
   float scale_log2e;
-  int rows, row_tiles;     // (sequence, head of the group) pairs of a KV head, tiles of 128 of them
+  int seqs, row_tiles;     // tiles of 128 (sequence, head of the group) pairs of a KV head
   int key0, n_blk, splits; // first key of the prefix that any sequence sees, blocks from there on, shares of them
   float *part_o, *part_ml;
   int max_parts;

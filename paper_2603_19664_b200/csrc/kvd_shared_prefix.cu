@@ -1,24 +1,25 @@
 // Attention of a batch to the prefix that its sequences share (include/kvd.h, kvd_shared_prefix_attention): Eq. 6-7 with the
 // prefix's keys and values read from memory once for the whole batch.
 //
-//   rows  = (sequence, head of the group) of one KV head, 128 per tile; a CTA takes NT tiles (two where there are two and
+//   rows  = (sequence, head of the group) of one KV head, 128 per tile (G = 3: 42 sequences, two rows stay empty); a CTA takes NT tiles (two where there are two and
 //           tensor memory holds both), a KV head and a share of the prefix, and leaves one partial (maximum, sum,
 //           unnormalised output) per row, which the merge kernel of decode attention joins with those of the sequence's own
 //           keys.
 //   keys  = blocks of BK (128, at d_head 256 64), K and V in turns through a ring that TMA fills (64-channel slabs, 128-byte
-//           swizzle; past the prefix's end it fills zeros, which are masked).
-//   S     = Q K^T into tensor memory, four warps per row tile: a thread has a row, takes its maximum and weights in
-//           registers, and puts the weights, in the element type, over the scores as the A operand of O += P V.
+//           swizzle; past the prefix's end it fills zeros, which are masked).  The query tiles come by TMA, too.
+//   S     = Q K^T into tensor memory, four warps per row tile: a thread has a row, takes its maximum, then its weights, 32 columns
+//           at a time, and puts the weights, in the element type, over the scores as the A operand of O += P V.
 //   order = one thread issues all products.  One row tile: two score buffers, S runs a block ahead of the softmax.  Two row
 //           tiles: one each, and a tile's products run during the other's softmax.
 //
 // Bound by reading the prefix as long as a block's arithmetic is shorter than its bytes take: per 128 keys of d_head 128 an
 // SM's share of memory is 2900 clocks, the products of two row tiles 2048.  The weights' reference moves only when a
 // block's maximum exceeds it by 2^8 (as in the prefill kernels), so O is rarely rescaled.
+//
+// The kernel leaves room on its SM -- registers, shared memory -- for CTAs of the streaming kernel that attends the sequences' own
+// keys: that kernel is launched behind this one and starts beside it (AttnLaunchHead::beside), the merge behind both.
 #include <math_constants.h>
 #include <string.h>
-
-#include <algorithm>
 
 #include "kvd_internal.h"
 #include "kvd_ptx.cuh"
@@ -40,11 +41,10 @@ struct SpCfg {
   static constexpr int COL_O = 0, COL_S = NT * D_HEAD;
   static constexpr int COLS_USED = COL_S + NT * S_BUFS * BK;
   static constexpr int COLS = COLS_USED <= 256 ? 256 : 512;
-  static constexpr int FREE = 232448 - 1024 - 1024 - NT * Q_BYTES;
-  static constexpr int SLOTS = FREE / BLOCK_BYTES < 8 ? FREE / BLOCK_BYTES : 8;
+  static constexpr int SLOTS = D_HEAD == 64 ? 6 : NT == 2 ? 3 : 4;  // (about half of shared memory, 60 KB to spare at d_head 256)
   static constexpr int N_BARS = 2 * SLOTS + NT * (2 * S_BUFS + 3);
   static constexpr int SMEM_BYTES = 1024 + NT * Q_BYTES + SLOTS * BLOCK_BYTES + N_BARS * 8;
-  static_assert(COLS_USED <= 512 && SLOTS >= 4, "does not fit");
+  static_assert(COLS_USED <= 512 && SLOTS >= 3, "does not fit");
 };
 
 __device__ __forceinline__ bool sp_wait(uint32_t bar, uint32_t parity, const volatile int *abort_flag, unsigned long long timeout_ns) {
@@ -66,11 +66,17 @@ __device__ __forceinline__ bool sp_warp_wait(uint32_t bar, uint32_t parity, cons
   return ok != 0;
 }
 
+struct SpMaps {
+  CUtensorMap q;     // [sequences][n_q][d_head], boxes of 64 channels, a group's heads and a tile's sequences
+  CUtensorMap k, v;  // [len][n_kv * d_head], boxes of 64 channels and a block's keys
+};
+
 template <int D_HEAD, int G, int DT, int NT>
 __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
-    kvd_shared_prefix_kernel(const __grid_constant__ SharedPrefixParams P, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+    kvd_shared_prefix_kernel(const __grid_constant__ SharedPrefixParams P, const __grid_constant__ SpMaps M) {
   using Cfg = SpCfg<D_HEAD, NT>;
   constexpr int BK = Cfg::BK, SLOTS = Cfg::SLOTS, S_BUFS = Cfg::S_BUFS;
+  constexpr int SEQS = SP_ROWS / G;  // sequences of a row tile (G = 3: 42, and two rows stay empty)
   extern __shared__ uint8_t sp_smem_raw[];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort_i;
@@ -105,12 +111,13 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
       }
       mbar_init(bar_pv_done(t), 1);
       mbar_init(bar_o(t), 1);
-      mbar_init(bar_q(t), 4);
+      mbar_init(bar_q(t), 1);
     }
     fence_mbar_init();
     s_abort_i = 0;
-    prefetch_tensormap(&map_k);
-    prefetch_tensormap(&map_v);
+    prefetch_tensormap(&M.q);
+    prefetch_tensormap(&M.k);
+    prefetch_tensormap(&M.v);
   }
   if (warp == 4 * NT) {
     tmem_claim(smem_u32(&s_tmem), Cfg::COLS);
@@ -118,32 +125,17 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  grid_launch_dependents();
+  // dependents are let in behind the wait: the streaming kernel relies on it that what precedes this kernel is complete
   grid_dependency_wait();
+  grid_launch_dependents();
   const uint32_t tmem_base = s_tmem;
 
   if (warp < 4 * NT) {
     // ------------------------------------------------------------------ softmax: thread = row
-    const int t = warp >> 2, q4 = warp & 3, in_tile = q4 * 32 + lane, row0 = (group * NT + t) * SP_ROWS, row = row0 + in_tile;
+    const int t = warp >> 2, q4 = warp & 3, in_tile = q4 * 32 + lane;
     const uint32_t lane_field = static_cast<uint32_t>(q4 * 32) << 16;
-    const bool valid = row < P.rows;
-    const int seq = valid ? row / G : 0, head = kvh * G + (valid ? row % G : 0);
-    // this warp's 32 rows of the query tile: 16-byte pieces, neighbouring lanes on neighbouring pieces
-    {
-      constexpr int CPR = D_HEAD / 8;
-#pragma unroll 4
-      for (int i = lane; i < 32 * CPR; i += 32) {
-        const int r = q4 * 32 + i / CPR, c = i % CPR, rr = row0 + r;
-        const bool have = rr < P.rows;
-        const __nv_bfloat16 *src = P.q + (have ? (static_cast<long long>(rr / G) * P.n_q + kvh * G + rr % G) * D_HEAD + c * 8 : 0);
-        cp_async16(q_smem + t * Cfg::Q_BYTES + (c >> 3) * Cfg::SLAB_Q + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, have);
-      }
-      cp_async_commit();
-      cp_async_wait_all();
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_q(t));
-    }
+    const bool valid = in_tile < SEQS * G && (group * NT + t) * SEQS + in_tile / G < P.seqs;
+    const int seq = valid ? (group * NT + t) * SEQS + in_tile / G : 0, head = kvh * G + (valid ? in_tile % G : 0);
     const int lo = valid ? P.lo[seq] : 0, hi = valid ? P.hi[seq] : -1;  // the prefix's keys that the row sees
     const int all_lo = __reduce_max_sync(0xffffffffu, valid ? lo : INT_MIN), all_hi = __reduce_min_sync(0xffffffffu, valid ? hi : INT_MAX);
     const uint64_t c2 = pack2(P.scale_log2e, P.scale_log2e), one2 = pack2(1.0f, 1.0f);
@@ -159,25 +151,28 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
         break;
       }
       tc_fence_after();
-      uint32_t s[BK / 32][32];
-#pragma unroll
-      for (int i = 0; i < BK / 32; ++i) tmem_ld_x32(s_col + i * 32, s[i]);
-      tmem_wait_ld();
-      if (!(k0 >= all_lo && k0 + BK - 1 <= all_hi)) {
-#pragma unroll
-        for (int i = 0; i < BK / 32; ++i)
+      const bool whole = k0 >= all_lo && k0 + BK - 1 <= all_hi;
+      auto scores_of = [&](int i, uint32_t (&s)[32]) {
+        tmem_ld_x32(s_col + i * 32, s);
+        tmem_wait_ld();
+        if (!whole) {
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if (k0 + i * 32 + k < lo || k0 + i * 32 + k > hi) s[i][k] = 0xff800000u;  // -inf
+            if (k0 + i * 32 + k < lo || k0 + i * 32 + k > hi) s[k] = 0xff800000u;  // -inf
+        }
+      };
+      float mx[2] = {-CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll 1
+      for (int i = 0; i < BK / 32; ++i) {
+        uint32_t s[32];
+        scores_of(i, s);
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+          mx[0] = fmax3(mx[0], __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+          mx[1] = fmax3(mx[1], __uint_as_float(s[k + 2]), __uint_as_float(s[k + 3]));
+        }
       }
-      float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-      for (int i = 0; i < BK / 32; ++i)
-#pragma unroll
-        for (int k = 0; k < 32; k += 8)
-#pragma unroll
-          for (int u = 0; u < 4; ++u) mx[u] = fmax3(mx[u], __uint_as_float(s[i][k + 2 * u]), __uint_as_float(s[i][k + 2 * u + 1]));
-      const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * P.scale_log2e;  // (scale > 0)
+      const float bm = fmaxf(mx[0], mx[1]) * P.scale_log2e;  // (scale > 0)
       const float m_new = m == -CUDART_INF_F ? bm : (bm > m + SP_TAU ? bm : m);
       const float mu = m_new == -CUDART_INF_F ? 0.f : m_new;
       const float alpha = m == -CUDART_INF_F ? 1.0f : ex2_approx(m - mu);  // while nothing has been seen O and l are 0
@@ -185,20 +180,19 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
       const uint64_t al2 = pack2(alpha, alpha), nm2 = pack2(-mu, -mu);
       l2[0] = fmul2(l2[0], al2);
       l2[1] = fmul2(l2[1], al2);
+#pragma unroll 1
+      for (int i = 0; i < BK / 32; ++i) {
+        uint32_t s[32], w[16];
+        scores_of(i, s);
 #pragma unroll
-      for (int i = 0; i < BK / 64; ++i) {
-        uint32_t w[32];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int k = 0; k < 32; k += 2) {
-            float e0, e1;
-            unpack2(ffma2(pack2(__uint_as_float(s[2 * i + h][k]), __uint_as_float(s[2 * i + h][k + 1])), c2, nm2), e0, e1);
-            const float p0 = ex2_approx(e0), p1 = ex2_approx(e1);
-            w[16 * h + (k >> 1)] = pack_out<DT>(p0, p1);
-            l2[(k >> 1) & 1] = ffma2(pack2(p0, p1), one2, l2[(k >> 1) & 1]);
-          }
-        tmem_st_x32(s_col + i * 32, w);  // over the scores, which are in registers
+        for (int k = 0; k < 32; k += 2) {
+          float e0, e1;
+          unpack2(ffma2(pack2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, nm2), e0, e1);
+          const float p0 = ex2_approx(e0), p1 = ex2_approx(e1);
+          w[k >> 1] = pack_out<DT>(p0, p1);
+          l2[(k >> 1) & 1] = ffma2(pack2(p0, p1), one2, l2[(k >> 1) & 1]);
+        }
+        tmem_st_x16(s_col + i * 16, w);  // over scores that have been read: columns 16 i .. of 32 i ..
       }
       if (__any_sync(0xffffffffu, alpha != 1.0f)) {
         // O holds the blocks before j; the last of those products must have finished (j >= 1 here: a maximum exists)
@@ -240,9 +234,8 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
         tmem_ld_x32(tmem_base + lane_field + Cfg::COL_O + t * D_HEAD + c * 32, r);
         tmem_wait_ld();
         if (store) {
-          uint4 *dst = reinterpret_cast<uint4 *>(P.part_o + at * D_HEAD + c * 32);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) dst[i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+          // (32 bytes at a time: whole sectors, whose halves would be written one by one otherwise)
+          store_row_piece<8>(reinterpret_cast<__nv_bfloat16 *>(P.part_o + at * D_HEAD + c * 32), r, true);
         }
       }
       float a0, a1, a2, a3;
@@ -308,6 +301,12 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
   } else if (lane == 0) {
     // ------------------------------------------------------------------ blocks into the ring (one thread)
     bool ok = true;
+    for (int t = 0; t < NT; ++t) {
+      mbar_arrive_expect_tx(bar_q(t), SEQS * G * D_HEAD * 2);
+#pragma unroll
+      for (int c = 0; c < D_HEAD / 64; ++c)
+        tma_load_3d(q_smem + t * Cfg::Q_BYTES + c * Cfg::SLAB_Q, &M.q, bar_q(t), c * 64, kvh * G, (group * NT + t) * SEQS);
+    }
     int e = 0;
     for (; e < 2 * n_blk; ++e) {
       const int slot = e % SLOTS;
@@ -319,11 +318,13 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
       const int key = key0 + (e >> 1) * BK;
 #pragma unroll
       for (int c = 0; c < D_HEAD / 64; ++c)
-        tma_load_2d(ring + slot * Cfg::BLOCK_BYTES + c * Cfg::SLAB, (e & 1) ? &map_v : &map_k, bar_full(slot), kvh * D_HEAD + c * 64, key);
+        tma_load_2d(ring + slot * Cfg::BLOCK_BYTES + c * Cfg::SLAB, (e & 1) ? &M.v : &M.k, bar_full(slot), kvh * D_HEAD + c * 64, key);
     }
     if (!ok) {
       raise(P.status, STATUS_TIMEOUT, s_abort);
       // the copies in flight land before the CTA's shared memory goes to another
+      const volatile int never = 0;
+      for (int t = 0; t < NT; ++t) sp_wait(bar_q(t), 0, &never, tmo);
       for (int i = e < SLOTS ? 0 : e - SLOTS; i < e; ++i) {
         const unsigned long long t0 = globaltimer_ns();
         while (!mbar_try_wait(bar_full(i % SLOTS), (i / SLOTS) & 1) && globaltimer_ns() - t0 < tmo) __nanosleep(20);
@@ -343,7 +344,7 @@ int shared_prefix_block(int d_head) { return d_head == 256 ? 64 : 128; }
 int shared_prefix_tiles(int d_head, int row_tiles) { return d_head <= 128 && row_tiles > 1 ? 2 : 1; }
 
 template <int D_HEAD, int G, int DT, int NT>
-static kvd_status sp_launch(kvd_ctx *ctx, const SharedPrefixParams &P, const CUtensorMap &map_k, const CUtensorMap &map_v, cudaStream_t stream) {
+static kvd_status sp_launch(kvd_ctx *ctx, const SharedPrefixParams &P, const SpMaps &M, cudaStream_t stream) {
   using Cfg = SpCfg<D_HEAD, NT>;
   auto kern = kvd_shared_prefix_kernel<D_HEAD, G, DT, NT>;
   static std::atomic<bool> configured[64] = {};
@@ -360,46 +361,52 @@ static kvd_status sp_launch(kvd_ctx *ctx, const SharedPrefixParams &P, const CUt
   attr[0].val.programmaticStreamSerializationAllowed = serial_launch_mask() & 2 ? 0 : 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kern, P, map_k, map_v);
+  e = cudaLaunchKernelEx(&cfg, kern, P, M);
   if (e != cudaSuccess) return cuda_fail(ctx, e, "launch shared prefix");
   ctx->launches += 1;
   return KVD_OK;
 }
 template <int D_HEAD, int G>
-static kvd_status sp_dtype(kvd_ctx *ctx, const SharedPrefixParams &P, const CUtensorMap &k, const CUtensorMap &v, cudaStream_t stream) {
+static kvd_status sp_dtype(kvd_ctx *ctx, const SharedPrefixParams &P, const SpMaps &M, cudaStream_t stream) {
   const bool f16 = ctx->dtype == KVD_DTYPE_F16;
   if constexpr (D_HEAD <= 128) {
-    if (shared_prefix_tiles(D_HEAD, P.row_tiles) == 2) return f16 ? sp_launch<D_HEAD, G, 1, 2>(ctx, P, k, v, stream) : sp_launch<D_HEAD, G, 0, 2>(ctx, P, k, v, stream);
+    if (shared_prefix_tiles(D_HEAD, P.row_tiles) == 2) return f16 ? sp_launch<D_HEAD, G, 1, 2>(ctx, P, M, stream) : sp_launch<D_HEAD, G, 0, 2>(ctx, P, M, stream);
   }
-  return f16 ? sp_launch<D_HEAD, G, 1, 1>(ctx, P, k, v, stream) : sp_launch<D_HEAD, G, 0, 1>(ctx, P, k, v, stream);
+  return f16 ? sp_launch<D_HEAD, G, 1, 1>(ctx, P, M, stream) : sp_launch<D_HEAD, G, 0, 1>(ctx, P, M, stream);
 }
 template <int D_HEAD>
-static kvd_status sp_group(kvd_ctx *ctx, const SharedPrefixParams &P, int group, const CUtensorMap &k, const CUtensorMap &v, cudaStream_t stream) {
+static kvd_status sp_group(kvd_ctx *ctx, const SharedPrefixParams &P, int group, const SpMaps &M, cudaStream_t stream) {
   switch (group) {
-    case 1: return sp_dtype<D_HEAD, 1>(ctx, P, k, v, stream);
-    case 2: return sp_dtype<D_HEAD, 2>(ctx, P, k, v, stream);
-    case 3: return sp_dtype<D_HEAD, 3>(ctx, P, k, v, stream);
-    case 4: return sp_dtype<D_HEAD, 4>(ctx, P, k, v, stream);
-    case 8: return sp_dtype<D_HEAD, 8>(ctx, P, k, v, stream);
+    case 1: return sp_dtype<D_HEAD, 1>(ctx, P, M, stream);
+    case 2: return sp_dtype<D_HEAD, 2>(ctx, P, M, stream);
+    case 3: return sp_dtype<D_HEAD, 3>(ctx, P, M, stream);
+    case 4: return sp_dtype<D_HEAD, 4>(ctx, P, M, stream);
+    case 8: return sp_dtype<D_HEAD, 8>(ctx, P, M, stream);
     default: return KVD_ERR_SHAPE;
   }
 }
 kvd_status launch_shared_prefix(kvd_ctx *ctx, const SharedPrefixParams &P, const kvd_kv_segment &prefix, int d_head, int group, cudaStream_t stream) {
-  CUtensorMap maps[2];
-  const int bk = shared_prefix_block(d_head);
-  for (int i = 0; i < 2; ++i) {
+  static thread_local SpMaps M;
+  const cuuint32_t ones[3] = {1, 1, 1};
+  const cuuint64_t q_dims[3] = {static_cast<cuuint64_t>(d_head), static_cast<cuuint64_t>(P.n_q), static_cast<cuuint64_t>(P.seqs)};
+  const cuuint64_t q_strides[2] = {static_cast<cuuint64_t>(d_head) * 2, static_cast<cuuint64_t>(P.n_q) * d_head * 2};
+  const cuuint32_t q_box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(SP_ROWS / group)};
+  bool ok = ctx->encode(&M.q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16 *>(P.q), q_dims, q_strides, q_box, ones,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  for (int i = 0; ok && i < 2; ++i) {
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(P.n_kv) * d_head, static_cast<cuuint64_t>(prefix.len)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(prefix.row_stride) * 2};
-    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(bk)}, ones[2] = {1, 1};
-    if (ctx->encode(&maps[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(i ? prefix.v : prefix.k), dims, strides, box, ones,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return KVD_ERR_SHAPE;
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(shared_prefix_block(d_head))};
+    ok = ctx->encode(i ? &M.v : &M.k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(i ? prefix.v : prefix.k), dims, strides, box, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   }
+  if (!ok) return KVD_ERR_SHAPE;
   switch (d_head) {
-    case 64: return sp_group<64>(ctx, P, group, maps[0], maps[1], stream);
-    case 128: return sp_group<128>(ctx, P, group, maps[0], maps[1], stream);
-    case 256: return sp_group<256>(ctx, P, group, maps[0], maps[1], stream);
+    case 64: return sp_group<64>(ctx, P, group, M, stream);
+    case 128: return sp_group<128>(ctx, P, group, M, stream);
+    case 256: return sp_group<256>(ctx, P, group, M, stream);
     default: return KVD_ERR_SHAPE;
   }
 }
