@@ -1072,16 +1072,24 @@ extern "C" kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int b
         P.key0 = lo_all;
         const int bk = shared_prefix_block(d.d_head), nt = shared_prefix_tiles(d.d_head, P.row_tiles);
         P.n_blk = (hi_all - lo_all) / bk + 1;
-        // as many shares of the prefix as fill the SMs once, as far as blocks and the workspace's slots go
+        // Shares of the prefix: one wave of CTAs at most, and as many as the workspace has slots for.  Fewer where the partials cost
+        // more than they save: the blocks of a CTA take 1.5 us each, of two row tiles 2.3, and the partials' way through memory and
+        // the merge goes at 1.25 MB/us (64 sequences behind 8192 keys, Qwen3-4B layer, 18 / 9 / 6 shares 45 / 38 / 39 us; 8 behind
+        // 32749, Gemma-3-4B layer, 37 / 18 shares 32 / 43).
         st = build_attn_launch(ctx, ls, b0, nb, q, q_pos, segs, n_segs, scale, out, nullptr, L);
         if (st != KVD_OK) return st;
         const int ctas = (P.row_tiles + nt - 1) / nt * d.n_kv_heads;
-        int splits = ctx->num_sms / ctas;
         const int room = (ctx->max_parts - L.total_chunks) / nb;
-        splits = splits < P.n_blk ? splits : P.n_blk;
-        splits = splits < room ? splits : room;
         if (room < 1) return KVD_ERR_CAPACITY;
-        P.splits = splits < 1 ? 1 : splits;
+        int most = ctx->num_sms / ctas;
+        most = most < P.n_blk ? most : P.n_blk;
+        most = most < room ? most : room;
+        const double block_us = nt == 2 ? 2.3 : 1.5, partial_us = static_cast<double>(nb) * d.n_q_heads * d.d_head * 8 / 1.25e6;
+        double best = 1e300;
+        for (int n = 1; n <= most || n == 1; ++n) {
+          const double t = block_us * ((P.n_blk + n - 1) / n) + partial_us * n;
+          if (t < best) best = t, P.splits = n;
+        }
       }
       for (int i = 0; i < nb; ++i) pre[i] = P.splits;
       st = build_attn_launch(ctx, ls, b0, nb, q, q_pos, segs, n_segs, scale, out, P.splits > 0 ? pre : nullptr, L, tails);

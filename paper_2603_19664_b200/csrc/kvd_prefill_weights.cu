@@ -32,7 +32,7 @@ constexpr int PW_ROWS = 128;      // query rows per tile
 constexpr int PW_KEYS = 128;      // keys per tile
 constexpr int PW_RANGE = 64;      // row tiles one CTA of the columns pass can take
 constexpr int PW_CHUNK = 8;       // key tiles of one (sums in shared memory)
-constexpr int PW_POLY = 3;        // of every eight pairs of scores, those that take the fp32 pipes
+constexpr int PW_POLY = 2;        // of every eight pairs of scores, those that take the fp32 pipes
 
 struct PwParams {
   const __nv_bfloat16 *q;  // [n_rows][n_q][d_head]
@@ -325,9 +325,12 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
       const int qp = valid ? max(P.q_pos[tok], -1) : -1, lo = first_visible(qp, P.window);
       // range that every stored row of the warp sees
       const int all_lo = __reduce_max_sync(0xffffffffu, valid ? lo : INT_MIN), all_hi = __reduce_min_sync(0xffffffffu, valid ? qp : INT_MAX);
+      // ... as far as the segment goes that held the last such piece
+      int whole_lo = 1, whole_hi = 0;
       // The reference m is the first finite maximum the row meets, rounded up to a whole number, and moves only if a sum
       // threatens to leave fp32's range: 2^(s - m) is as exact for any m.
       float m = valid ? -CUDART_INF_F : 0.f, l = 0.f;  // (rows that nobody filled score anything)
+      bool seen = false;  // every row of the warp has a reference
       for (int j = turn; j < n_blk; j += TURNS) {
         const int buf = j % S_BUFS, pos0 = (t0 + j) * PW_KEYS + half * 64;
         if (!pw_warp_wait(bar_s_full(buf), (j / S_BUFS) & 1, s_abort, tmo, lane)) {
@@ -336,7 +339,15 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
           break;
         }
         tc_fence_after();
-        const bool whole = pos0 >= all_lo && pos0 + 63 <= all_hi && pw_held(P, pos0, 64);
+        if (pos0 < whole_lo || pos0 + 63 > whole_hi) {
+#pragma unroll
+          for (int sg = 0; sg < KVD_MAX_SEGMENTS; ++sg)
+            if (segment_holds(P.first[sg], P.len[sg], pos0, 64)) {
+              whole_lo = max(P.first[sg], all_lo);
+              whole_hi = min(P.first[sg] + P.len[sg] - 1, all_hi);
+            }
+        }
+        const bool whole = pos0 >= whole_lo && pos0 + 63 <= whole_hi;
         unsigned long long vis = ~0ull;
         if (!whole) {
           vis = 0ull;
@@ -360,9 +371,10 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
             for (int k = 0; k < 32; ++k)
               if (!((v >> k) & 1u)) s[k] = 0xff800000u;  // -inf
           }
-          if (__any_sync(0xffffffffu, m == -CUDART_INF_F)) {
+          if (!seen) {  // (uniform)
             const float bm = ceilf(pw_max32(s) * P.scale_log2e);
             if (m == -CUDART_INF_F) m = bm;
+            seen = !__any_sync(0xffffffffu, m == -CUDART_INF_F);
           }
           const float mu = m == -CUDART_INF_F ? 0.f : m;
           const uint64_t nm2 = pack2(-mu, -mu);
@@ -657,25 +669,25 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
   }
 }
 
-// out_p = in_p + the partial columns of position p: 32 positions per CTA, eight warps over the partials, added in order.
-__global__ void __launch_bounds__(256) kvd_prefill_weights_sum_kernel(const __grid_constant__ PwParams P) {
+// out_p = in_p + the partial columns of position p: 32 positions per CTA, PW_SUM warps over the partials, added in order.
+constexpr int PW_SUM = 32;
+__global__ void __launch_bounds__(PW_SUM * 32) kvd_prefill_weights_sum_kernel(const __grid_constant__ PwParams P) {
   grid_launch_dependents();
   grid_dependency_wait();
-  __shared__ float s_part[8][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, p = static_cast<int>(blockIdx.x) * 32 + lane;
+  __shared__ float s_part[PW_SUM][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, p = static_cast<int>(blockIdx.x) * 32 + lane, warps = static_cast<int>(blockDim.x) >> 5;
   const int n = P.ranges * P.n_kv;
   const long long width = static_cast<long long>(P.key_tiles) * PW_KEYS, col = p - static_cast<long long>(P.key_tile0) * PW_KEYS;
   float sum = 0.f;
   if (p < P.n_positions && col >= 0 && col < width) {
 #pragma unroll 8
-    for (int i = warp; i < n; i += 8) sum += __ldcg(P.cols + i * width + col);
+    for (int i = warp; i < n; i += warps) sum += __ldcg(P.cols + i * width + col);
   }
   s_part[warp][lane] = sum;
   __syncthreads();
   if (warp == 0 && p < P.n_positions) {
     float w = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w += s_part[i][lane];
+    for (int i = 0; i < warps; ++i) w += s_part[i][lane];
     P.out[p] = (P.in ? P.in[p] : 0.f) + w;
   }
 }
@@ -699,8 +711,8 @@ static double pw_estimate(int d_head, long long ctas, double rows, double tiles,
   if (ctas <= PW_PLAN_SMS) return one;  // (the longest one has all of its tiles)
   const double full = one - tiles * tile + tiles * tile_sm * per_sm;  // beside another one
   if (share > 0.9) return full * ((ctas + per_sm * PW_PLAN_SMS - 1) / (per_sm * PW_PLAN_SMS));
-  // uneven work (causal calls, windows): long CTAs start first, and half of one is under way when the others are done
-  return ctas * share * ((PW_START + rows * PW_SWITCH) / per_sm + tiles * tile_sm) / PW_PLAN_SMS + 0.5 * full;
+  // uneven work (causal calls, windows): long CTAs start first, and a third of one is left when the others are done
+  return ctas * share * ((PW_START + rows * PW_SWITCH) / per_sm + tiles * tile_sm) / PW_PLAN_SMS + 0.35 * full;
 }
 // seen_tiles: of the key tiles, those a row tile can see; share: of all pairs of tiles, those that see each other.
 static PwPlan pw_plan(int d_head, int n_kv, int group, int n_rows, int key_tiles, int seen_tiles, double share) {
@@ -756,7 +768,9 @@ static kvd_status pw_launch(kvd_ctx *ctx, const PwParams &P, const PwMaps &M, cu
   };
   launch(rows, static_cast<long long>(P.row_tiles) * P.n_kv * P.splits, R::THREADS, R::SMEM_BYTES, M);
   launch(columns, static_cast<long long>(P.chunks) * P.ranges * P.n_kv, C::THREADS, C::SMEM_BYTES, M);
-  launch(kvd_prefill_weights_sum_kernel, (P.n_positions + 31ll) / 32, 256, 0);
+  // a warp for every eight partials, eight loads at once (fewer partials: eight warps)
+  const int partials = P.ranges * P.n_kv, sum_warps = partials >= 8 * PW_SUM ? PW_SUM : partials >= 64 ? (partials + 7) / 8 : 8;
+  launch(kvd_prefill_weights_sum_kernel, (P.n_positions + 31ll) / 32, 32 * sum_warps, 0);
   return e == cudaSuccess ? KVD_OK : cuda_fail(ctx, e, "launch prefill weights");
 }
 template <int D_HEAD>
@@ -838,7 +852,7 @@ extern "C" kvd_status kvd_prefill_attention_weights(kvd_ctx *ctx, int layer, int
   if (n_rows == 0 || P.seg_hi < 0) {  // nothing weighs anything
     P.key_tile0 = P.key_tiles = P.ranges = 0;
     if (weights_in == weights_out) return KVD_OK;
-    kvd_prefill_weights_sum_kernel<<<(n_positions + 31) / 32, 256, 0, stream>>>(P);
+    kvd_prefill_weights_sum_kernel<<<(n_positions + 31) / 32, 32, 0, stream>>>(P);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(ctx, e, "launch prefill weights (sum)");
     ctx->launches += 1;
