@@ -972,7 +972,7 @@ static kvd_status build_attn_launch(kvd_ctx *ctx, const LayerState &ls, int b0, 
   // (counted as if all live keys were streamed: what is refused does not hang on which kernel takes them)
   if (streamed_slots > ctx->max_parts) return KVD_ERR_CAPACITY;
   const float sc = scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(d.d_head));
-  L.beside = false;
+  L.beside = L.stream_only = false;
   L.n_seqs = nb;
   L.total_chunks = parts;
   L.n_q = d.n_q_heads;
@@ -1074,7 +1074,7 @@ extern "C" kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int b
         P.n_blk = (hi_all - lo_all) / bk + 1;
         // Shares of the prefix: one wave of CTAs at most, and as many as the workspace has slots for.  Fewer where the partials cost
         // more than they save: the blocks of a CTA take 1.5 us each, of two row tiles 2.3, and the partials' way through memory and
-        // the merge goes at 1.25 MB/us (64 sequences behind 8192 keys, Qwen3-4B layer, 18 / 9 / 6 shares 45 / 38 / 39 us; 8 behind
+        // the merge goes at 1.25 MB/us (64 sequences behind 8192 keys, Qwen3-4B layer, 18 / 9 / 6 shares 41 / 36 / 37 us; 8 behind
         // 32749, Gemma-3-4B layer, 37 / 18 shares 32 / 43).
         st = build_attn_launch(ctx, ls, b0, nb, q, q_pos, segs, n_segs, scale, out, nullptr, L);
         if (st != KVD_OK) return st;
@@ -1110,7 +1110,9 @@ extern "C" kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int b
         if (st != KVD_OK) return st;
       }
       L.beside = P.splits > 0;
+      L.stream_only = P.splits > 0 && shared_prefix_merges(ctx, L, d.d_head);
       st = launch_attention(ctx, L, d.d_head, group, stream);
+      if (st == KVD_OK && L.stream_only) st = launch_shared_merge(ctx, L, d.d_head, stream);
       if (st != KVD_OK) return st;
     }
   return KVD_OK;

@@ -1035,6 +1035,7 @@ static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t str
     }
     if (e != cudaSuccess) return e;
   }
+  if (S.stream_only) return cudaSuccess;
   attr[0].val.programmaticStreamSerializationAllowed = ((small || S.early) && !(serial_launch_mask() & 4)) ? 1 : 0;
   // as many warps per merge CTA as the longest sequence of the launch has groups of partials
   int merge_warps = 1;
@@ -1098,7 +1099,7 @@ static kvd_status launch_attn_impl(kvd_ctx *ctx, const AttnLaunch &L, cudaStream
     cudaError_t e = ctx->dtype == 1 ? attn_launch_pair<D_HEAD, G, NSEQ, 1, ATTN_WEIGH>(S, stream, weigh)
                                     : attn_launch_pair<D_HEAD, G, NSEQ, 0, ATTN_WEIGH>(S, stream, weigh);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "launch attention");
-    ctx->launches += L.total_chunks > 0 ? 2 : 1;
+    ctx->launches += (L.total_chunks > 0 ? 1 : 0) + (L.stream_only ? 0 : 1);
   }
   return KVD_OK;
 }
@@ -1308,7 +1309,7 @@ extern "C" kvd_status kvd_decode_attention_static(int n_q_heads, int n_kv_heads,
   L.part_o = reinterpret_cast<float *>(scratch + ml_bytes);
   L.status = nullptr;
   L.max_parts = parts;
-  L.early = L.tail = L.beside = false;
+  L.early = L.tail = L.beside = L.stream_only = false;
   switch (d_head) {
     case 64: return static_launch_d<64>(L, group, stream);
     case 128: return static_launch_d<128>(L, group, stream);

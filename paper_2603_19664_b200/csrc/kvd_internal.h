@@ -204,6 +204,7 @@ struct AttnLaunchHead {
   int max_parts;           // slots the partial arrays hold
   bool early;              // both kernels start early whatever their grids
   bool beside;             // behind the shared prefix's kernel: the streaming kernel starts beside it, the merge waits for both
+  bool stream_only;        // the merge is somebody else's
   bool tail;               // there is a sequence whose live keys the merge kernel attends itself (attn_tail)
   float *scores;           // launches that weigh their keys: [n_seqs][n_q][score_stride], column 0 = chunk0_pos (log2 units)
   long long score_stride;  // even
@@ -450,6 +451,15 @@ struct SharedPrefixParams {
 };
 int shared_prefix_block(int d_head);                         // keys per block
 int shared_prefix_tiles(int d_head, int row_tiles);          // row tiles per CTA
+// its merge, for launches of many rows (shared_prefix_merges says which)
+struct SharedMergeParams {
+  const float *part_o, *part_ml;
+  __nv_bfloat16 *out;
+  int n_seqs, n_q;
+  int base[AT_MAX_SEQS], count[AT_MAX_SEQS];  // a sequence's slots
+};
+bool shared_prefix_merges(const kvd_ctx *ctx, const AttnLaunch &L, int d_head);
+kvd_status launch_shared_merge(kvd_ctx *ctx, const AttnLaunch &L, int d_head, cudaStream_t stream);
 kvd_status launch_shared_prefix(kvd_ctx *ctx, const SharedPrefixParams &P, const kvd_kv_segment &prefix, int d_head, int group, cudaStream_t stream);
 // kvd_prefill_attention: many query tokens of one sequence, tiled over query rows (Eq. 6-7 per row)
 struct PrefillParams {

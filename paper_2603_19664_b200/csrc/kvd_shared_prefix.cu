@@ -339,6 +339,96 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
   }
 }
 
+// Merge of a launch of many rows with a few dozen partials each, a thread for four channels of a row: the partials in slot
+// order, eight at a time, with a running maximum.  (The merge of decode attention gives a CTA to a head group and a slice of
+// channels, whose registers leave three CTAs on an SM: 64 sequences of 32 heads of 128, 21 partials each, 13 us.)
+constexpr int SP_MERGE_THREADS = 256;
+template <int D_HEAD, int DT>
+__global__ void __launch_bounds__(SP_MERGE_THREADS) kvd_shared_merge_kernel(const __grid_constant__ SharedMergeParams P) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  constexpr int PER_ROW = D_HEAD / 4, BATCH = 8;
+  const int at = static_cast<int>(blockIdx.x) * SP_MERGE_THREADS + static_cast<int>(threadIdx.x), row = at / PER_ROW, c = at % PER_ROW;
+  if (row >= P.n_seqs * P.n_q) return;
+  const int seq = row / P.n_q, head = row % P.n_q, count = P.count[seq];
+  const size_t first = static_cast<size_t>(P.base[seq]) * P.n_q + head;
+  const float2 *ml = reinterpret_cast<const float2 *>(P.part_ml) + first;
+  const float4 *po = reinterpret_cast<const float4 *>(P.part_o + first * D_HEAD) + c;
+  float m = -CUDART_INF_F, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = 0; p0 < count; p0 += BATCH) {
+    float2 x[BATCH];
+    float4 v[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const size_t off = static_cast<size_t>(p0 + i < count ? p0 + i : count - 1) * P.n_q;
+      x[i] = __ldcg(ml + off);
+      v[i] = __ldcg(po + off * PER_ROW);
+      if (p0 + i >= count) x[i].x = -CUDART_INF_F;
+    }
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) mn = fmaxf(mn, x[i].x);
+    const float mu = mn == -CUDART_INF_F ? 0.f : mn, f = exp2f(m - mu);
+    m = mn;
+    l *= f;
+    o.x *= f;
+    o.y *= f;
+    o.z *= f;
+    o.w *= f;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const float w = exp2f(x[i].x - mu);
+      if (p0 + i >= count) continue;
+      l = fmaf(w, x[i].y, l);
+      o.x = fmaf(w, v[i].x, o.x);
+      o.y = fmaf(w, v[i].y, o.y);
+      o.z = fmaf(w, v[i].z, o.z);
+      o.w = fmaf(w, v[i].w, o.w);
+    }
+  }
+  const float r = l > 0.f ? 1.0f / l : 0.f;  // (nothing seen: zeros)
+  reinterpret_cast<uint2 *>(P.out)[at] = make_uint2(pack_out<DT>(o.x * r, o.y * r), pack_out<DT>(o.z * r, o.w * r));
+}
+// Where a wave of such CTAs is there to be filled, and no live keys are left to the merge.
+bool shared_prefix_merges(const kvd_ctx *ctx, const AttnLaunch &L, int d_head) {
+  return !L.tail && static_cast<long long>(L.n_seqs) * L.n_q * (d_head / 4) >= static_cast<long long>(ctx->num_sms) * SP_MERGE_THREADS;
+}
+kvd_status launch_shared_merge(kvd_ctx *ctx, const AttnLaunch &L, int d_head, cudaStream_t stream) {
+  static thread_local SharedMergeParams P;
+  P.part_o = L.part_o;
+  P.part_ml = L.part_ml;
+  P.out = L.out;
+  P.n_seqs = L.n_seqs;
+  P.n_q = L.n_q;
+  for (int i = 0; i < L.n_seqs; ++i) {
+    if (L.seq[i].merge_base < 0 || L.seq[i].merge_base + L.seq[i].merge_count > L.max_parts) return KVD_ERR_CAPACITY;
+    P.base[i] = L.seq[i].merge_base;
+    P.count[i] = L.seq[i].merge_count;
+  }
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.stream = stream;
+  cfg.gridDim = dim3((L.n_seqs * L.n_q * (d_head / 4) + SP_MERGE_THREADS - 1) / SP_MERGE_THREADS, 1, 1);
+  cfg.blockDim = dim3(SP_MERGE_THREADS, 1, 1);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = serial_launch_mask() & 4 ? 0 : 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const bool f16 = ctx->dtype == KVD_DTYPE_F16;
+  cudaError_t e;
+  switch (d_head) {
+    case 64: e = f16 ? cudaLaunchKernelEx(&cfg, kvd_shared_merge_kernel<64, 1>, P) : cudaLaunchKernelEx(&cfg, kvd_shared_merge_kernel<64, 0>, P); break;
+    case 128: e = f16 ? cudaLaunchKernelEx(&cfg, kvd_shared_merge_kernel<128, 1>, P) : cudaLaunchKernelEx(&cfg, kvd_shared_merge_kernel<128, 0>, P); break;
+    case 256: e = f16 ? cudaLaunchKernelEx(&cfg, kvd_shared_merge_kernel<256, 1>, P) : cudaLaunchKernelEx(&cfg, kvd_shared_merge_kernel<256, 0>, P); break;
+    default: return KVD_ERR_SHAPE;
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "launch shared merge");
+  ctx->launches += 1;
+  return KVD_OK;
+}
+
 // Blocks of keys and the row tiles of a CTA, by head size.
 int shared_prefix_block(int d_head) { return d_head == 256 ? 64 : 128; }
 int shared_prefix_tiles(int d_head, int row_tiles) { return d_head <= 128 && row_tiles > 1 ? 2 : 1; }

@@ -17,7 +17,7 @@ for _f in ("kvd_prefill_weights.cu", "kvd_shared_prefix.cu", "kvd_evict.cu", "kv
             i += 1
         KERNELS[_m.group(1)] = (_m.group(2), _text[_m.end():i])
 NEW = ["kvd_prefill_weights_kernel", "kvd_prefill_weights_sum_kernel", "kvd_shared_prefix_kernel", "kvd_evict_select_kernel",
-       "kvd_evict_rows_kernel", "kvd_attn_merge_weigh_kernel"]
+       "kvd_evict_rows_kernel", "kvd_shared_merge_kernel", "kvd_attn_merge_weigh_kernel"]
 
 
 @pytest.mark.parametrize("name", NEW)
