@@ -18,6 +18,9 @@
  *                            over the CONCAT of up to four position-contiguous K/V segments
  *                            (recomputed, live window, current token), grouped-query heads,
  *                            optional sliding-window mask.
+ *   kvd_shared_prefix_attention, kvd_decode_attention_weights, kvd_prefill_attention_weights, kvd_cache_evict
+ *                            attention of a batch behind one prefix, what every cached key has weighed, and
+ *                            eviction by that: the window of Algorithm 1 chosen by weight instead of by age.
  *
  * General rules
  *   - Plain C.  Every pointer documented as DEVICE points to memory on the context's GPU that the
@@ -394,7 +397,10 @@ kvd_status kvd_prefill_attention(kvd_ctx *ctx, int layer, int n_rows, const void
  * sequence's own in the merge.  prefix->len == 0 is kvd_decode_attention.  The split of the prefix depends on the batch and
  * its weights are rounded to the element type before the second product, so the bits are not those of kvd_decode_attention
  * (same tolerance against the definition), and a sequence's bits may depend on the batch's size.  The prefix must not
- * overlap a sequence's own segments in position.  n_segs <= KVD_MAX_SEGMENTS.  Needs an attached workspace. */
+ * overlap a sequence's own segments in position.  Where sequences see the prefix in part (a sliding window, a query inside
+ * it), a value that is not finite reaches the sequences that do not see it as well (0 times infinity), if they see another
+ * key of its block of 128 (64 at d_head 256).  n_segs <= KVD_MAX_SEGMENTS.  bf16 and fp16 contexts; needs an attached
+ * workspace. */
 kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int batch, const void *q, const int32_t *q_pos,
                                        const kvd_kv_segment *prefix, const kvd_kv_segment *segs, int n_segs, float scale,
                                        void *out, void *stream);
@@ -413,7 +419,7 @@ kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int batch, const
  * KVD_ERR_CAPACITY when a visible key's position is >= n_positions (at most 2^30).  scratch: DEVICE, 256-byte aligned, at
  * least kvd_weights_scratch_bytes(desc, batch, span) for the longest visible span of a sequence; the scores pass through it.
  * A head whose row of scores is all minus infinity adds nothing; a NaN among a head's scores makes the weights of its keys
- * NaN.  Heads are added in ascending order: equal calls give equal bits. */
+ * NaN.  Heads are added in ascending order: equal calls give equal bits.  bf16 and fp16 contexts. */
 size_t kvd_weights_scratch_bytes(const kvd_model_desc *desc, int batch, int max_span);
 kvd_status kvd_decode_attention_weights(kvd_ctx *ctx, int layer, int batch, const void *q, const int32_t *q_pos,
                                         const kvd_kv_segment *segs, int n_segs, float scale, void *out,

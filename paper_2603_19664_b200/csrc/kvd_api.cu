@@ -1143,7 +1143,7 @@ extern "C" kvd_status kvd_decode_attention_weights(kvd_ctx *ctx, int layer, int 
   if (!q || !q_pos || !out || !weights_out || !scratch || (n_segs > 0 && !segs)) return KVD_ERR_INVALID_ARG;
   if (n_positions < 0 || weights_stride < n_positions) return KVD_ERR_INVALID_ARG;
   if (n_positions > (1 << 30)) return KVD_ERR_CAPACITY;
-  if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return KVD_ERR_ALIGNMENT;
+  if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0 || !aligned4({weights_in, weights_out})) return KVD_ERR_ALIGNMENT;
   const kvd_model_desc &d = ctx->desc;
   if (batch > d.max_batch) return KVD_ERR_CAPACITY;
   const int group = d.n_q_heads / d.n_kv_heads;

@@ -50,7 +50,7 @@ struct EvictParams {
   int len[EV_MAX_SEQS], protect_from[EV_MAX_SEQS];
 };
 
-static_assert(6 * EV_BINS >= EV_RUN, "a single CTA's holes");
+static_assert(12 * EV_BINS >= EV_RUN, "a single CTA's holes: at most half of its slots");
 struct EvictShared {
   uint32_t hist[3][EV_BINS];    // this CTA's counts, by pass; a single CTA's holes after that
   uint32_t sum[3][EV_BINS];     // rank 0: the cluster's, added up by remote atomics
@@ -399,6 +399,7 @@ extern "C" kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_
   if (max_len > KVD_MAX_EVICT_SLOTS || max_kept > out->slots || max_gone > evicted_stride) return KVD_ERR_CAPACITY;
   if (max_gone > 0 && !evicted_out) return KVD_ERR_INVALID_ARG;
   if (max_len == 0) return KVD_OK;
+  if (!aligned4({in->weights, in->positions, out->weights, out->positions, slots_out, evicted_out})) return KVD_ERR_ALIGNMENT;
   if (rows) {
     if (in->row_stride < kdim || out->row_stride < kdim) return KVD_ERR_INVALID_ARG;
     const uintptr_t p = reinterpret_cast<uintptr_t>(in->k) | reinterpret_cast<uintptr_t>(in->v) | reinterpret_cast<uintptr_t>(out->k) | reinterpret_cast<uintptr_t>(out->v);

@@ -9,6 +9,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <initializer_list>
 #include <map>
 #include <string>
 #include <vector>
@@ -481,6 +482,12 @@ struct PrefillParams {
 kvd_status launch_prefill_tc(kvd_ctx *ctx, const PrefillParams &P, int d_head, int group, cudaStream_t stream);
 kvd_status launch_selftest_timeout(kvd_ctx *ctx, unsigned long long timeout_ns, cudaStream_t stream);
 kvd_status cuda_fail(kvd_ctx *ctx, cudaError_t e, const char *where);
+// fp32 and int32 arrays of the caller's (NULL is aligned)
+inline bool aligned4(std::initializer_list<const void *> ps) {
+  uintptr_t bits = 0;
+  for (const void *p : ps) bits |= reinterpret_cast<uintptr_t>(p);
+  return (bits & 3u) == 0;
+}
 // host helpers shared by the entry points (kvd_api.cu)
 kvd_status encode_2d(kvd_ctx *ctx, CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer,
                      uint32_t box_inner, uint32_t box_outer, int eb = 2);

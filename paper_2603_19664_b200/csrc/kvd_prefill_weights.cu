@@ -815,7 +815,8 @@ extern "C" kvd_status kvd_prefill_attention_weights(kvd_ctx *ctx, int layer, int
   if (ctx->dtype == KVD_DTYPE_F32) return KVD_ERR_UNSUPPORTED;
   if (n_positions == 0 && n_segs == 0) return KVD_OK;
   if (!weights_out || !scratch || (n_segs > 0 && !segs) || (n_rows > 0 && (!q || !q_pos))) return KVD_ERR_INVALID_ARG;
-  if ((reinterpret_cast<uintptr_t>(q) & 15u) != 0 || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return KVD_ERR_ALIGNMENT;
+  if ((reinterpret_cast<uintptr_t>(q) & 15u) != 0 || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0 || !aligned4({q_pos, weights_in, weights_out}))
+    return KVD_ERR_ALIGNMENT;
   if (n_positions > (1 << 30)) return KVD_ERR_CAPACITY;
   const kvd_model_desc &d = ctx->desc;
   const int kdim = d.n_kv_heads * d.d_head, group = d.n_q_heads / d.n_kv_heads;

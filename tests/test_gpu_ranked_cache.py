@@ -336,6 +336,24 @@ def test_evict_the_longest_cache_and_the_lists_alone():
         assert torch.equal(k[i, :17], k0[i][torch.tensor(want, device="cuda")])
 
 
+def test_evict_rows_of_an_fp32_context():
+    nq, nkv, dh = SHAPES["smollm2"]
+    ctx = kvd.Kvd(kvd.make_desc(1, 64, nq, nkv, dh, 1e-6, False, 1e-6))
+    ctx.kvd_set_dtype(2)
+    g, row = gen(22), nkv * dh
+    k, v, pos, w = cache_of(g, 2, 300, row + 4, "plain", torch.float32)
+    k0, w0, p0 = k.clone(), w.clone(), pos.clone()
+    slots, gone = torch.empty((2, 300), dtype=torch.int32, device="cuda"), torch.empty((2, 300), dtype=torch.int32, device="cuda")
+    cache = (k, v, pos, w, row + 4, 300)
+    ctx.kvd_cache_evict(2, cache, [300, 299], 100, 0, None, cache, slots, gone, 300)
+    assert ctx.kvd_poll_status() == kvd.KVD_OK
+    for i, n in enumerate((300, 299)):
+        want, _ = evict_plain(w0[i].tolist(), p0[i].tolist(), n, 100, 0, 2**31)
+        at = torch.tensor(want, device="cuda")
+        assert slots[i, :100].tolist() == want and torch.equal(k[i, :100, :row], k0[i][at][:, :row])
+        assert torch.equal(k[i, :, row:], k0[i, :, row:])  # what lies between the rows stays
+
+
 # ------------------------------------------------------------------------------------------------ shared prefix
 @pytest.mark.parametrize("shape,dtype", [("smollm2", 0), ("gemma", 0), ("gemma", 1), ("qwen", 0), ("qwen", 1), ("g1", 0), ("g8", 0), ("g8-256", 0)])
 @pytest.mark.parametrize("batch,prefix,first,own", [(1, 1, 0, 1), (3, 127, 0, 9), (5, 1000, 3, 200), (40, 2500, 0, 30), (70, 300, 0, 5)])
@@ -445,6 +463,8 @@ def test_refusals():
     refused(B.KVD_ERR_INVALID_ARG, dec, 0, 2, q, [63, 63], segs, 0.0, out, None, w, 32, 64, scratch)       # rows shorter than their positions
     refused(B.KVD_ERR_CAPACITY, dec, 0, 2, q, [63, 63], segs, 0.0, out, None, w, 64, 64, scratch[:256])
     refused(B.KVD_ERR_ALIGNMENT, dec, 0, 2, q, [63, 63], segs, 0.0, out, None, w, 64, 64, scratch[16:])
+    odd = torch.zeros(1024, dtype=torch.uint8, device="cuda")[2:]
+    refused(B.KVD_ERR_ALIGNMENT, dec, 0, 2, q, [63, 63], segs, 0.0, out, odd, w, 64, 64, scratch)
     refused(B.KVD_ERR_INVALID_ARG, dec, 1, 2, q, [63, 63], segs, 0.0, out, None, w, 64, 64, scratch)       # no such layer
     refused(B.KVD_ERR_CAPACITY, dec, 0, 5, q, [63] * 5, segs + segs + segs[:1], 0.0, out, None, w, 64, 64, scratch)
     pos = torch.zeros(2, dtype=torch.int32, device="cuda")
@@ -477,7 +497,15 @@ def test_refusals():
     refused(B.KVD_ERR_CAPACITY, ev, 1, (None, None, None, big, 0, 131073), [131073], 10, 0, None, (None, None, None, None, 0, 64),
             lists[0], torch.empty((1, 131073), dtype=torch.int32, device="cuda"), 131073)
     assert ctx.kvd_launch_count() == launches and bool((out == 5.0).all()) and bool((w == 5.0).all())
-    f32, _ = open_ctx("smollm2")
+    refused(B.KVD_ERR_ALIGNMENT, ev, 2, cache[:3] + (odd, row, 64), [64, 64], 10, 0, None, other, *lists, 64)
+    assert ctx.kvd_launch_count() == launches
+    f32 = kvd.Kvd(kvd.make_desc(1, 64, nq, nkv, dh, 1e-6, False, 1e-6))
+    f32.kvd_set_dtype(2)
+    f32.kvd_set_layer(0, torch.zeros((64, 2 * row), device="cuda"), torch.ones(64, device="cuda"), None, 1e4)
+    f32.kvd_attach_workspace(torch.empty(kvd.kvd_workspace_bytes(f32.desc), dtype=torch.uint8, device="cuda"))
+    refused(B.KVD_ERR_UNSUPPORTED, f32.kvd_shared_prefix_attention, 0, 1, q, [70], prefix, [[]], 0.0, out)
+    refused(B.KVD_ERR_UNSUPPORTED, f32.kvd_decode_attention_weights, 0, 1, q, [63], segs[:1], 0.0, out, None, w, 64, 64, scratch)
+    refused(B.KVD_ERR_UNSUPPORTED, f32.kvd_prefill_attention_weights, 0, 2, q, pos, segs[0], 0.0, None, w[0], 64, s2)
     fresh = kvd.Kvd(kvd.make_desc(1, 64, nq, nkv, dh, 1e-6, False, 1e-6))
     refused(B.KVD_ERR_STATE, fresh.kvd_shared_prefix_attention, 0, 1, q, [70], prefix, [[]], 0.0, out)
     assert kvd.kvd_weights_scratch_bytes(desc, 0, 5) == 0 and kvd.kvd_prefill_weights_scratch_bytes(desc, 1, 0) == 0
