@@ -29,6 +29,8 @@ constexpr int EV_BATCH = 8;                       // slots whose loads a thread 
 constexpr int EV_MAX_CTAS = 8;                    // a portable cluster
 constexpr int EV_CTA_SLOTS = KVD_MAX_EVICT_SLOTS / EV_MAX_CTAS;
 constexpr int EV_RUN = 8192;                      // slots that one CTA is enough for
+constexpr int EV_SMALL = 2048;                    // slots up to which the rows are moved in the same launch
+constexpr int EV_SMALL_BYTES = 128 << 10;         // ... if a CTA has no more to read than this
 constexpr uint32_t EV_PROTECTED = 0xffffffffu;    // above the key of plus infinity, 0xff800000
 constexpr uint32_t EV_GONE = 0x80000000u, EV_MOVES = 0x40000000u;
 constexpr int EV_MAX_SEQS = 64;
@@ -50,6 +52,7 @@ struct EvictParams {
   int len[EV_MAX_SEQS], protect_from[EV_MAX_SEQS];
 };
 
+static_assert(3 * EV_BINS >= EV_SMALL, "places of a small cache");
 static_assert(12 * EV_BINS >= EV_RUN, "a single CTA's holes: at most half of its slots");
 struct EvictShared {
   uint32_t hist[3][EV_BINS];    // this CTA's counts, by pass; a single CTA's holes after that
@@ -73,14 +76,15 @@ __device__ __forceinline__ void add_cluster_u32(uint32_t addr, uint32_t v) {
   asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 
-__global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const __grid_constant__ EvictParams P, int ctas) {
+__global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const __grid_constant__ EvictParams P, int ctas, int copies) {
   extern __shared__ __align__(16) uint8_t ev_smem[];
   EvictShared &S = *reinterpret_cast<EvictShared *>(ev_smem);
   uint32_t *ev_keys = reinterpret_cast<uint32_t *>(ev_smem + sizeof(EvictShared));  // [run], and the slots' positions behind them
   int32_t *ev_pos = reinterpret_cast<int32_t *>(ev_keys + P.run);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = ctas > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  const int b = static_cast<int>(blockIdx.x) / ctas;
+  // (copies > 1: each CTA of the cluster takes all of the sequence's slots, comes to the same result, and moves a share of the rows)
+  const int rank = ctas > 1 ? static_cast<int>(cluster_ctarank()) : 0, copy = copies > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int b = static_cast<int>(blockIdx.x) / (ctas * copies);
   const int len = P.len[b], keep = P.keep < len ? P.keep : len;
   const int slot0 = rank * P.run, n = max(0, min(P.run, len - slot0));
   auto all_sync = [&]() {
@@ -122,6 +126,7 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
       }
     }
   }
+  if (copies > 1) cluster_sync_all();  // everyone has read what the first of them may overwrite
   // ---- T: the keep-th largest key; need: how many of the slots equal to it stay
   uint32_t T, need;
   auto select = [&]() {
@@ -270,7 +275,7 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
   }
   // The r-th hole is the r-th evicted slot.  Its mover learns of it from shared memory (where the counts were), in a cluster from
   // the evicted list, which gets its positions once all have asked.
-  uint32_t *holes = &S.hist[0][0];
+  uint32_t *holes = &S.hist[0][0], *source = &S.sum[0][0];  // (source: the slot that goes to a place, where rows are moved here)
   int32_t *ev = P.evicted_out + b * P.evicted_stride;
 #pragma unroll 4
   for (int t = 0; t < turns; ++t) {
@@ -305,11 +310,13 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
       dst[u] = static_cast<int>(what);  // (negative: gone)
       if ((what & (EV_GONE | EV_MOVES)) == EV_MOVES) dst[u] = !KVD_BOUNDS_OK(r < len - keep, P.status) ? keep : ctas > 1 ? __ldcg(ev + r) : static_cast<int>(holes[r]);
       if (i >= n) dst[u] = keep;
-      x[u] = dst[u] >= 0 && i < n && P.weights_out ? w[slot0 + i] : 0.f;
+      x[u] = dst[u] >= 0 && i < n && P.weights_out && copy == 0 ? w[slot0 + i] : 0.f;
     }
 #pragma unroll
     for (int u = 0; u < EV_BATCH; ++u) {
       const int i = at + u * EV_THREADS;
+      if (copies > 1 && dst[u] >= 0 && dst[u] < keep) source[dst[u]] = static_cast<uint32_t>(i);
+      if (copy != 0) continue;
       if (dst[u] < 0) {
         if (ctas == 1 && KVD_BOUNDS_OK((dst[u] & 0x7fffffff) < len - keep, P.status)) ev[dst[u] & 0x7fffffff] = ev_pos[i];
       } else if (dst[u] < keep) {
@@ -318,6 +325,33 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
         if (P.weights_out) P.weights_out[b * P.cap_out + dst[u]] = x[u];
       }
     }
+  }
+  if (copies > 1) {
+    // the rows: a warp for each, K and V, the CTAs of the sequence in turns
+    __syncthreads();
+    const uint4 *k = P.k + b * P.cap_in * P.row_in, *v = P.v + b * P.cap_in * P.row_in;
+    uint4 *k_out = P.k_out + b * P.cap_out * P.row_out, *v_out = P.v_out + b * P.cap_out * P.row_out;
+    for (int dst = copy + copies * warp; dst < keep; dst += copies * EV_WARPS) {
+      const int src = static_cast<int>(source[dst]);
+      if (P.k == P.k_out && src == dst) continue;
+      if (!KVD_BOUNDS_OK(src >= 0 && src < len, P.status)) continue;
+      for (int c0 = lane; c0 < P.row_chunks; c0 += 128) {
+        uint4 x[2][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c0 + 32 * u < P.row_chunks) {
+            x[0][u] = k[src * P.row_in + c0 + 32 * u];
+            x[1][u] = v[src * P.row_in + c0 + 32 * u];
+          }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c0 + 32 * u < P.row_chunks) {
+            k_out[dst * P.row_out + c0 + 32 * u] = x[0][u];
+            v_out[dst * P.row_out + c0 + 32 * u] = x[1][u];
+          }
+      }
+    }
+    return;
   }
   if (ctas == 1) return;
   cluster_sync_all();
@@ -433,6 +467,11 @@ extern "C" kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_
   P.row_in = rows ? in->row_stride * eb / 16 : 0;
   P.row_out = rows ? out->row_stride * eb / 16 : 0;
   P.row_chunks = static_cast<int>(kdim * eb / 16);
+  // Small caches: one launch instead of two, the selection made by every CTA of a cluster for itself, the rows shared out.
+  int copies = 1;
+  if (rows && max_len <= EV_SMALL)
+    while (copies < EV_MAX_CTAS && 2 * copies * batch <= ctx->num_sms) copies *= 2;
+  if (static_cast<int64_t>(max_kept) * kdim * eb * 2 > static_cast<int64_t>(copies) * EV_SMALL_BYTES) copies = 1;
   P.rows_per_cta = (4 * EV_ROW_THREADS + P.row_chunks - 1) / P.row_chunks;
   P.status = ctx->d_status;
   for (int b0 = 0; b0 < batch; b0 += EV_MAX_SEQS) {
@@ -455,20 +494,20 @@ extern "C" kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_
     memset(&cfg, 0, sizeof(cfg));
     cudaLaunchAttribute attr[2];
     cfg.stream = stream;
-    cfg.gridDim = dim3(nb * ctas, 1, 1);
+    cfg.gridDim = dim3(nb * ctas * copies, 1, 1);
     cfg.blockDim = dim3(EV_THREADS, 1, 1);
     cfg.dynamicSmemBytes = smem;
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = (serial_launch_mask() & 8) || 2 * nb * ctas > ctx->num_sms ? 0 : 1;
+    attr[0].val.programmaticStreamSerializationAllowed = (serial_launch_mask() & 8) || 2 * nb * ctas > ctx->num_sms ? 0 : 1;  // (as launch_dependent)
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.x = ctas * copies;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = ctas > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, kvd_evict_select_kernel, P, ctas);
+    cfg.numAttrs = ctas * copies > 1 ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kvd_evict_select_kernel, P, ctas, copies);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "launch evict (select)");
     ctx->launches += 1;
-    if (!rows || max_kept == 0) continue;
+    if (!rows || max_kept == 0 || copies > 1) continue;
     const int tiles = (max_kept + P.rows_per_cta - 1) / P.rows_per_cta;
     cfg.gridDim = dim3(nb * tiles, 1, 1);
     cfg.blockDim = dim3(EV_ROW_THREADS, 1, 1);
