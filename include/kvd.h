@@ -462,7 +462,7 @@ typedef struct {
  *   evicted_out DEVICE int32 [batch][evicted_stride]: the positions of the evicted keys, by ascending slot (what
  *               kvd_recompute_kv rebuilds from the residual store when they are needed after all); lens[b] - keep entries
  *               are written, evicted_stride holds the most of them (KVD_ERR_CAPACITY).  NULL only when nothing is evicted.
- * lens[b] <= KVD_MAX_EVICT_SLOTS.  Two launches; nothing is launched when any argument is rejected. */
+ * lens[b] <= KVD_MAX_EVICT_SLOTS.  One launch for small caches, two for others; nothing is launched when any argument is rejected. */
 kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_cache *in, const int32_t *lens, int keep,
                            int32_t protect_below, const int32_t *protect_from, const kvd_ranked_cache *out,
                            int32_t *slots_out, int32_t *evicted_out, int64_t evicted_stride, void *stream);

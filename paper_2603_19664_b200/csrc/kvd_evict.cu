@@ -7,9 +7,15 @@
 // digit at which the count from above passes what is still wanted.  Slots above T stay, and of those equal to T as many of
 // the lowest as are wanted.
 //
-// One cluster per sequence, its slots dealt out in contiguous runs that stay in shared memory, so that memory is read once.
-// Histograms of the CTAs are added up in the shared memory of rank 0 (integer additions: their order changes nothing), every
-// CTA scans the sum itself; ranks among kept, evicted and moved slots are prefix counts, over threads, warps and CTAs.
+// One CTA per sequence of up to EV_RUN slots, a cluster beyond, its slots dealt out in contiguous runs that stay in shared
+// memory, so that memory is read once.  Histograms of a cluster's CTAs are added up in the shared memory of rank 0 (integer
+// additions: their order changes nothing), every CTA scans the sum itself; ranks among kept, evicted and moved slots are prefix
+// counts: a warp owns a run of slots, keeps what concerns them as masks of a turn's 32 lanes, and counts bits.
+//
+// Selecting is a chain of barriers (8192 slots, 14 us before ranks were counted from masks: keys 2.3, digits 2.9, ranks 5,
+// lists 3.6; 10 to 12 since): splitting it over a cluster's CTAs shortens the walks and lengthens the barriers.  us for the call, 8 x 8192
+// slots of a Qwen3-4B layer to 2001, one CTA 35, clusters of 2 / 4 / 8 37 / 38 / 42; 1 x 32768 of a SmolLM2 layer, clusters of
+// 2 / 4 / 8 31 / 25 / 27.  Moving rows is a copy, 5.8 TB/s (132 MB, 22.7 us).
 //
 // Slots below `keep` that stay keep their place; the r-th evicted slot below `keep` (a hole) receives the r-th kept slot
 // from `keep` on (a mover).  So an eviction in place moves as few keys as possible, and no key is read that the same call
@@ -467,7 +473,10 @@ extern "C" kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_
   P.row_in = rows ? in->row_stride * eb / 16 : 0;
   P.row_out = rows ? out->row_stride * eb / 16 : 0;
   P.row_chunks = static_cast<int>(kdim * eb / 16);
-  // Small caches: one launch instead of two, the selection made by every CTA of a cluster for itself, the rows shared out.
+  // Small caches: one launch instead of two, the selection made by every CTA of a cluster for itself, the rows shared out: as
+  // long as a CTA's share is short, since a few CTAs' loads in flight are far from the memory's rate.  us, two launches / one,
+  // three quarters kept: SmolLM2 layer 1 x 256 9.1 / 7.5, 1 x 1024 10.2 / 9.9, 1 x 2048 11.1 / 12.5, 8 x 1024 10.6 / 10.2, 40 x 256
+  // 10.4 / 9.5, 40 x 1024 18.8 / 20.9, 8 x 3000 15.1 / 17.0; Qwen3-4B layer 8 x 256 9.8 / 9.4, 1 x 1024 9.9 / 16.2, 8 x 2048 26.0 / 27.4.
   int copies = 1;
   if (rows && max_len <= EV_SMALL)
     while (copies < EV_MAX_CTAS && 2 * copies * batch <= ctx->num_sms) copies *= 2;

@@ -18,6 +18,11 @@
 // Two CTAs share an SM, so that one's start and end pass behind the other's work (d_head 256, whose tiles fill shared memory:
 // one CTA with twice the warps).  In a CTA eight (sixteen) warps take exponentials, one issues products, one fetches tiles.
 // Every wait is bounded, as in the other tensor-core kernels.
+//
+// Bound by exponentials and what surrounds them.  4096 tokens of a Qwen3-4B layer: rows 92, columns 120, sum 6 us; one product
+// alone would be 42, a pass's exponentials at 16 per clock and SM 69 at 1.7 GHz (three quarters of them: 52).  With an eighth of the exponentials the passes take 65
+// and 74.  One persistent CTA per SM instead, each key tile against two row tiles, with sixteen warps for exponentials and one or
+// two for products, takes 59 and 68 then, but 94 and 127 with all of them.
 #include <math_constants.h>
 #include <string.h>
 
@@ -32,7 +37,9 @@ constexpr int PW_ROWS = 128;      // query rows per tile
 constexpr int PW_KEYS = 128;      // keys per tile
 constexpr int PW_RANGE = 64;      // row tiles one CTA of the columns pass can take
 constexpr int PW_CHUNK = 8;       // key tiles of one (sums in shared memory)
-constexpr int PW_POLY = 2;        // of every eight pairs of scores, those that take the fp32 pipes
+// Of every eight pairs of scores, those that take the fp32 pipes.  Rows / columns pass of 4096 tokens of a Qwen3-4B layer with 0,
+// 1, 2, 3 of them: 91 / 116, 89 / 119, 90 / 116, 96 / 126 us (special-function units busy 56 % / 43 % with two; issue slots 60 %).
+constexpr int PW_POLY = 2;
 
 struct PwParams {
   const __nv_bfloat16 *q;  // [n_rows][n_q][d_head]

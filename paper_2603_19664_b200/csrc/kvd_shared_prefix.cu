@@ -18,6 +18,9 @@
 //
 // The kernel leaves room on its SM -- registers, shared memory -- for CTAs of the streaming kernel that attends the sequences' own
 // keys: that kernel is launched behind this one and starts beside it (AttnLaunchHead::beside), the merge behind both.
+//
+// Alone: 32749 keys of a Gemma-3-4B layer (fp16, 8 sequences) 30 us, 134 MB at 4.5 TB/s; 8192 keys of a Qwen3-4B layer (64 sequences)
+// 26.5 us with 64 CTAs, 18.8 with 144, whose partials cost the merge more (13.2 against 5.6 us) than they save beside the own keys' 24.
 #include <math_constants.h>
 #include <string.h>
 
