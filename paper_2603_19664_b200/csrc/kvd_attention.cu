@@ -867,9 +867,9 @@ __global__ void __launch_bounds__(AT_MERGE_THREADS)
 // position that the query does not see or that nobody holds keeps its weight; a head whose keys all score minus infinity
 // adds nothing.
 //
-// Bound by memory as the streaming kernel is: 16 x 8192 keys of a Qwen3-4B layer 115 us against 106 without weights, 17 MB of scores
+// Bound by memory as the streaming kernel is: 16 x 8192 keys of a Qwen3-4B layer 113 us against 106 without weights, 17 MB of scores
 // written and read beside 520 MB of K and V; this launch 21 us, of which the merge alone takes most.  (A merge CTA per query
-// head 122; the CTAs of the weights first 113, but a SmolLM2 step of 100 keys 8.0 instead of 7.8.)
+// head: 122.)
 template <int NSEQ>
 __device__ __forceinline__ void attn_weigh_cta(const AttnLaunchT<NSEQ> &P, const AttnWeigh &W, int block) {
   extern __shared__ float at_merge_smem[];  // per head: -(m + log2 l), or minus infinity for a head that adds nothing
@@ -946,15 +946,18 @@ __device__ __forceinline__ void attn_weigh_cta(const AttnLaunchT<NSEQ> &P, const
   W.out[at] = (W.in ? W.in[at] : 0.f) + w0;
   if (p + 1 < W.n_positions) W.out[at + 1] = (W.in ? W.in[at + 1] : 0.f) + w1;
 }
-// The merge of a launch that weighs its keys: merge CTAs first, then those of the weights.
+// The merge of a launch that weighs its keys.  In a launch of more CTAs than SMs those of the weights, which take longer, come
+// first (16 x 8192 keys of a Qwen3-4B layer 110.5 -> 108.9 us for the call), in a smaller one the merge's, whose output is waited for
+// (a SmolLM2 step of 100 keys 7.8 us, the other way 8.0).
 template <int D_HEAD, int G, int NSEQ, int DT, int GH>
 __global__ void __launch_bounds__(AT_MERGE_THREADS)
     kvd_attn_merge_weigh_kernel(const __grid_constant__ AttnLaunchT<NSEQ> P, const __grid_constant__ AttnWeigh W) {
   grid_launch_dependents();
   grid_dependency_wait();
-  const int merges = static_cast<int>(gridDim.x) - P.n_seqs * W.tiles;
-  if (static_cast<int>(blockIdx.x) < merges) attn_merge_cta<D_HEAD, G, NSEQ, DT, GH, false>(P, static_cast<int>(blockIdx.x));
-  else attn_weigh_cta<NSEQ>(P, W, static_cast<int>(blockIdx.x) - merges);
+  const int weighs = P.n_seqs * W.tiles, merges = static_cast<int>(gridDim.x) - weighs;
+  const int block = static_cast<int>(blockIdx.x), other = W.first ? weighs : merges;
+  if ((block < other) != W.first) attn_merge_cta<D_HEAD, G, NSEQ, DT, GH, false>(P, W.first ? block - weighs : block);
+  else attn_weigh_cta<NSEQ>(P, W, W.first ? block : block - merges);
 }
 
 // dynamic shared memory of the kernel and its one-time opt-in (sizes above 48 KB need it); the device's SMs
@@ -1066,6 +1069,7 @@ static cudaError_t attn_launch_pair(const AttnLaunchT<NSEQ> &S, cudaStream_t str
       W.tiles = (W.n_positions + 64 * merge_warps - 1) / (64 * merge_warps);
       const size_t merge_smem = (merge_warps * (AT_MERGE_SLICE + 1) + 2) * GH * sizeof(float), weigh_smem = S.n_q * sizeof(float);
       cfg.gridDim = dim3(S.n_seqs * ((S.n_q / GH) * (D_HEAD / AT_MERGE_SLICE) + W.tiles), 1, 1);
+      W.first = cfg.gridDim.x > static_cast<unsigned>(num_sms);
       cfg.dynamicSmemBytes = merge_smem > weigh_smem ? merge_smem : weigh_smem;
       return cudaLaunchKernelEx(&cfg, kvd_attn_merge_weigh_kernel<D_HEAD, G, NSEQ, DT, GH>, S, W);
     }

@@ -217,6 +217,7 @@ struct AttnWeigh {
   long long stride;
   int n_positions;
   int tiles;  // CTAs per sequence
+  bool first;  // ... ahead of the merge's in the grid
 };
 template <int NSEQ>
 struct AttnLaunchT : AttnLaunchHead {
