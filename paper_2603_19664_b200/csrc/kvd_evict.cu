@@ -214,6 +214,9 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kvd_evict_select_kernel(const _
         ev_keys[i] = key;
         atomicAdd(&S.hist[0][key >> 21], 1u);
       }
+      // (the weights were read again: once more everyone has to be done before the first CTA writes them.  T is the same in all
+      // CTAs of a cluster, so all of them are here.)
+      if (copies > 1) cluster_sync_all();
       select();
     }
   }

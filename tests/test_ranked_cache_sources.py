@@ -1,0 +1,33 @@
+"""What the sources of the ranked cache have to hold for races and sizes that no run shows (no GPU)."""
+import os
+import re
+
+import pytest  # noqa: F401
+
+from test_ranked_cache_rules import CSRC, KERNELS
+
+
+def _block(text, at):
+    """The text of the brace block that opens at or after `at`."""
+    at = text.index("{", at)
+    depth, i = 1, at + 1
+    while depth:
+        depth += {"{": 1, "}": -1}.get(text[i], 0)
+        i += 1
+    return text[at:i]
+
+
+def test_no_weight_is_read_once_a_cta_of_the_cluster_may_write_it():
+    """In the one-launch form every CTA of a cluster reads all of a sequence's weights and the first one writes them back, in
+    place to where others read: behind the last read that all of them make there is a barrier of the cluster."""
+    body = KERNELS["kvd_evict_select_kernel"][1]
+    barrier = "if (copies > 1) cluster_sync_all();"
+    write = body.index("P.weights_out[")
+    reads = [m.start() for m in re.finditer(r"\bw\[slot0 \+ i\]", body) if "copy == 0" not in body[body.rindex("\n", 0, m.start()):m.start()]]
+    assert len(reads) == 2 and max(reads) < write
+    again = _block(body, body.index("if (T == EV_PROTECTED)"))
+    for text in (body[:body.index("if (T == EV_PROTECTED)")], again):
+        read = max(m.end() for m in re.finditer(r"\bw\[slot0 \+ i\]", text))
+        assert barrier in text[read:]
+    # (a barrier that only some CTAs reached would hang: the branch hangs on T alone, which all of them find from the same keys)
+    assert "rank" not in again and "copy " not in again
