@@ -383,11 +383,19 @@ Segment = Tuple[object, object, int, int, int]  # (k tensor/ptr, v tensor/ptr, r
 KVD_STATIC_SCRATCH_BYTES = 8 << 20
 
 
+def _int32s(n: int, values, what: str):
+    """int32[n] (at least one).  ctypes fills an array up with zeros: fewer values than n are refused like more of them."""
+    ints = [int(x) for x in values]
+    if len(ints) < n:
+        raise IndexError(f"{what}: {len(ints)} values for {n}")
+    return (ctypes.c_int32 * max(n, 1))(*ints)
+
+
 def _marshal_segments(batch: int, q_pos, segs):
     """(segments per sequence, positions, kvd_kv_segment[batch][n_segs]).  One struct.pack of all fields: a structure
     field set from Python costs 0.15 us (64 sequences of one segment: 137 against 70 us)."""
     n_segs = max(map(len, segs), default=0)
-    pos_arr = (ctypes.c_int32 * max(batch, 1))(*[int(p) for p in q_pos])
+    pos_arr = _int32s(batch, q_pos, "q_pos")
     try:
         flat: List[int] = []
         for b in range(batch):
@@ -549,7 +557,7 @@ class Kvd:
                                        rows_out_row_stride, stream)
         if st < 0:
             arr = _marshal_ranges(ranges)
-            seqs = None if append_seqs is None else (ctypes.c_int32 * max(len(append_seqs), 1))(*[int(x) for x in append_seqs])
+            seqs = None if append_seqs is None else _int32s(max(n_rows, len(append_seqs)), append_seqs, "append_seqs")
             st = self._lib.kvd_decode_step_kv(self._h, layer, arr, len(ranges), out_row_stride, _ptr(rows), _ptr(positions), n_rows, seqs,
                                               _ptr(k_rows_out), _ptr(v_rows_out), rows_out_row_stride, stream)
         self._check(st, "kvd_decode_step_kv")
@@ -567,7 +575,7 @@ class Kvd:
                                   scale: float, out, stream=None) -> None:
         """Several query rows of one sequence (segs: that sequence's segments), each with its own position."""
         n_segs, _, seg_arr = _marshal_segments(1, [0], [list(segs)])
-        pos_arr = (ctypes.c_int32 * max(n_rows, 1))(*[int(p) for p in q_pos])
+        pos_arr = _int32s(n_rows, q_pos, "q_pos")
         self._check(self._lib.kvd_decode_attention_rows(self._h, layer, n_rows, _ptr(q), pos_arr, seg_arr, n_segs,
                                                         float(scale), _ptr(out), _stream(stream)),
                     "kvd_decode_attention_rows")
@@ -631,10 +639,9 @@ class Kvd:
         st = _calls.kvd_cache_evict(self._addr, batch, cache, lens, keep, protect_below, protect_from, cache_out, slots_out, evicted_out,
                                     evicted_stride, stream)
         if st < 0:
-            n = max(batch, 1)
             a, b = _marshal_cache(cache), _marshal_cache(cache_out)
-            len_arr = (ctypes.c_int32 * n)(*[int(x) for x in lens])
-            from_arr = None if protect_from is None else (ctypes.c_int32 * n)(*[int(x) for x in protect_from])
+            len_arr = _int32s(batch, lens, "lens")
+            from_arr = None if protect_from is None else _int32s(batch, protect_from, "protect_from")
             st = self._lib.kvd_cache_evict(self._h, batch, ctypes.byref(a), len_arr, keep, protect_below, from_arr, ctypes.byref(b), _ptr(slots_out),
                                            _ptr(evicted_out), evicted_stride, stream)
         self._check(st, "kvd_cache_evict")
