@@ -439,7 +439,8 @@ kvd_status kvd_prefill_attention_weights(kvd_ctx *ctx, int layer, int n_rows, co
                                          void *stream);
 
 /* Caches of a batch, `slots` keys of room each (DEVICE; element (slot j, head h, channel c) of sequence b's keys at
- * k[(b * slots + j) * row_stride + h * d_head + c], in the context's element type; positions and weights [batch][slots]). */
+ * k[(b * slots + j) * row_stride + h * d_head + c], in the context's element type; positions and weights [batch][slots]).  Keys
+ * and values may be columns of one buffer (v = k + n_kv_heads * d_head, row_stride at least twice that). */
 typedef struct {
   void *k;
   void *v;

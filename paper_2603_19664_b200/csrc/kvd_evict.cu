@@ -417,6 +417,18 @@ static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
 }
+// Rows of `width` bytes, `stride` apart.  Rows of one stride may lie between each other: keys and values as columns of one buffer.
+struct EvictRows {
+  const void *at;
+  size_t rows, stride, width;
+};
+static bool overlap(const EvictRows &a, const EvictRows &b) {
+  if (a.rows == 0 || b.rows == 0 || !overlap(a.at, (a.rows - 1) * a.stride + a.width, b.at, (b.rows - 1) * b.stride + b.width)) return false;
+  if (a.stride != b.stride) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  const size_t col = y >= x ? (y - x) % a.stride : (a.stride - (x - y) % a.stride) % a.stride;  // where b's columns begin in a's rows
+  return col < a.width || col + b.width > a.stride;
+}
 
 extern "C" kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_cache *in, const int32_t *lens, int keep, int32_t protect_below,
                                       const int32_t *protect_from, const kvd_ranked_cache *out, int32_t *slots_out, int32_t *evicted_out,
@@ -448,11 +460,14 @@ extern "C" kvd_status kvd_cache_evict(kvd_ctx *ctx, int batch, const kvd_ranked_
     const uintptr_t p = reinterpret_cast<uintptr_t>(in->k) | reinterpret_cast<uintptr_t>(in->v) | reinterpret_cast<uintptr_t>(out->k) | reinterpret_cast<uintptr_t>(out->v);
     if ((p & 15u) != 0 || in->row_stride * eb % 16 != 0 || out->row_stride * eb % 16 != 0) return KVD_ERR_ALIGNMENT;
     // in place: the same arrays with the same strides; otherwise nothing that is written may be read
-    const size_t nin = (static_cast<size_t>(batch - 1) * in->slots + max_len) * in->row_stride * eb, nout = (static_cast<size_t>(batch - 1) * out->slots + max_kept) * out->row_stride * eb;
+    const size_t nin = static_cast<size_t>(batch - 1) * in->slots + max_len, nout = max_kept > 0 ? static_cast<size_t>(batch - 1) * out->slots + max_kept : 0;
+    auto rows_of = [&](const void *p, const kvd_ranked_cache *c, size_t n) {
+      return EvictRows{p, n, static_cast<size_t>(c->row_stride) * eb, static_cast<size_t>(kdim) * eb};
+    };
+    const EvictRows ik = rows_of(in->k, in, nin), iv = rows_of(in->v, in, nin), ok = rows_of(out->k, out, nout), ov = rows_of(out->v, out, nout);
     const bool same = in->k == out->k && in->v == out->v && in->row_stride == out->row_stride && in->slots == out->slots;
-    if (!same && (overlap(in->k, nin, out->k, nout) || overlap(in->k, nin, out->v, nout) || overlap(in->v, nin, out->k, nout) || overlap(in->v, nin, out->v, nout)))
-      return KVD_ERR_INVALID_ARG;
-    if (overlap(out->k, nout, out->v, nout)) return KVD_ERR_INVALID_ARG;
+    if (!same && (overlap(ik, ok) || overlap(ik, ov) || overlap(iv, ok) || overlap(iv, ov))) return KVD_ERR_INVALID_ARG;
+    if (overlap(ok, ov)) return KVD_ERR_INVALID_ARG;
   }
   const size_t win = (static_cast<size_t>(batch - 1) * in->slots + max_len) * 4, wout = (static_cast<size_t>(batch - 1) * out->slots + max_kept) * 4;
   if (out->weights && !(out->weights == in->weights && out->slots == in->slots) && overlap(in->weights, win, out->weights, wout)) return KVD_ERR_INVALID_ARG;

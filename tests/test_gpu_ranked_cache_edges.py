@@ -57,3 +57,76 @@ def test_evict_among_protected_slots(cap, protected, kind):
         assert torch.equal(to[0][:, :keep], want_k) and torch.equal(to[1][:, :keep], want_v) and torch.equal(to[2][:, :keep], want_pos)
         assert torch.equal(to[3][:, :keep].view(torch.int32), want_w.view(torch.int32))
     torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------------ keys and values in one buffer
+@pytest.mark.parametrize("dtype", [0, 2])
+@pytest.mark.parametrize("cap,keep", [(300, 100), (5000, 1234)])
+def test_evict_keys_and_values_of_one_buffer(dtype, cap, keep):
+    """Rows that hold a token's key and its value, as the attention and rebuild calls take them: in place, into another such
+    buffer, into one with the halves the other way round and into its second half of the slots."""
+    nq, nkv, dh = SHAPES["smollm2"]
+    ctx = kvd.Kvd(kvd.make_desc(1, 64, nq, nkv, dh, 1e-6, False, 1e-6))
+    if dtype:
+        ctx.kvd_set_dtype(dtype)
+    dt = {0: torch.bfloat16, 2: torch.float32}[dtype]
+    g, row, b = gen(cap), nkv * dh, 2
+    stride = 2 * row + 16
+    kv0 = rnd(g, b, 2 * cap, stride, dtype=dt)
+    w = torch.rand((b, 2 * cap), generator=g, device="cuda")
+    lens = [cap, cap - 3]
+    want = [evict_plain(w[i].tolist(), list(range(2 * cap)), lens[i], keep, 4, 2**31) for i in range(b)]
+    at = torch.tensor([x[0] for x in want], device="cuda")
+
+    def rows_of(kv, first):
+        return kv.gather(1, at[..., None].expand(b, keep, stride))[..., first:first + row]
+
+    for form in ("in place", "another", "swapped", "behind"):
+        kv = kv0.clone()
+        cache = (kv, kv[:, :, row:], None, w, stride, 2 * cap)
+        if form == "in place":
+            to, ko, vo = cache[:2] + (None, None) + cache[4:], kv[:, :keep, :row], kv[:, :keep, row:2 * row]
+        elif form == "behind":  # (one sequence: its rows end where the others begin)
+            cache, to = (kv, kv[:, :, row:], None, w, stride, cap), (kv[0, cap:], kv[0, cap:, row:], None, None, stride, cap)
+            ko, vo = kv[:1, cap:cap + keep, :row], kv[:1, cap:cap + keep, row:2 * row]
+        else:
+            other = torch.full_like(kv, 5.0)
+            a, c = (0, row) if form == "another" else (row, 0)
+            to = (other[:, :, a:], other[:, :, c:], None, None, stride, 2 * cap)
+            ko, vo = other[:, :keep, a:a + row], other[:, :keep, c:c + row]
+        n = 1 if form == "behind" else b
+        slots, gone = torch.empty((b, 2 * cap), dtype=torch.int32, device="cuda"), torch.empty((b, 2 * cap), dtype=torch.int32, device="cuda")
+        ctx.kvd_cache_evict(n, cache, lens[:n], keep, 4, None, to, slots, gone, 2 * cap)
+        assert ctx.kvd_poll_status() == kvd.KVD_OK
+        assert torch.equal(ko, rows_of(kv0, 0)[:n]) and torch.equal(vo, rows_of(kv0, row)[:n])
+        if form == "in place":
+            assert torch.equal(kv[:, :, 2 * row:], kv0[:, :, 2 * row:]) and torch.equal(kv[:, keep:], kv0[:, keep:])
+        elif form == "behind":
+            assert torch.equal(kv[:, :cap], kv0[:, :cap]) and torch.equal(kv[1:], kv0[1:])
+        else:
+            assert bool((other[:, :, 2 * row:] == 5.0).all()) and bool((other[:, keep:] == 5.0).all()) and torch.equal(kv, kv0)
+
+
+def test_evict_refuses_rows_that_do_overlap():
+    nq, nkv, dh = SHAPES["smollm2"]
+    ctx = kvd.Kvd(kvd.make_desc(1, 64, nq, nkv, dh, 1e-6, False, 1e-6))
+    row = nkv * dh
+    kv, w = torch.zeros((2, 128, 2 * row), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 128), device="cuda")
+    lists = (torch.empty((2, 128), dtype=torch.int32, device="cuda"), torch.empty((2, 128), dtype=torch.int32, device="cuda"))
+    other = torch.zeros_like(kv)
+    launches = ctx.kvd_launch_count()
+
+    def no(cache, to):
+        refused(B.KVD_ERR_INVALID_ARG, ctx.kvd_cache_evict, 2, cache, [64, 64], 10, 0, None, to, *lists, 128)
+
+    whole = (kv, kv[:, :, row:], None, w, 2 * row, 64)
+    no(whole, (other, other[:, :, row - 8:], None, None, 2 * row, 64))           # the value's columns begin in the key's
+    no(whole, (other, other[:, :, 2 * row - 8:], None, None, 2 * row, 64))       # ... or end in the next key's
+    no(whole, (other, other, None, None, 2 * row, 64))
+    no(whole, (kv[:, :, row:], other, None, None, 2 * row, 64))                  # the cache's values as keys
+    no(whole, (other, kv[:, 1:], None, None, 2 * row, 64))                       # its keys, a row on
+    no(whole, (kv, kv[:, :, row:], None, None, 2 * row, 60))                     # in place with other strides
+    no(whole, (kv[:, 8:], kv[:, 8:, row:], None, None, 2 * row, 64))
+    no((kv, other, None, w, 2 * row, 64), (kv[:, :, row - 8:], torch.zeros_like(kv), None, None, 2 * row, 64))
+    no((kv, other, None, w, row, 64), (kv[:, 32:], torch.zeros_like(kv), None, None, 2 * row, 64))  # other strides over the same rows
+    assert ctx.kvd_launch_count() == launches
