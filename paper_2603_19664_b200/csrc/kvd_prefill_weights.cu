@@ -870,11 +870,13 @@ extern "C" kvd_status kvd_prefill_attention_weights(kvd_ctx *ctx, int layer, int
   P.key_tile0 = P.seg_lo / PW_KEYS;
   P.key_tiles = P.seg_hi / PW_KEYS - P.key_tile0 + 1;
   // (a window hides all but so many tiles from a row tile whose tokens follow each other)
-  const int row_span = (PW_ROWS + group - 1) / group, seen = ls.window > 0 ? (ls.window + row_span) / PW_KEYS + 2 : P.key_tiles;
+  const int row_span = (PW_ROWS + group - 1) / group;
+  const int64_t reach = ls.window > 0 ? (static_cast<int64_t>(ls.window) + row_span) / PW_KEYS + 2 : P.key_tiles;  // (windows go up to INT32_MAX)
+  const int seen = reach < P.key_tiles ? static_cast<int>(reach) : P.key_tiles;
   // (if the rows are the last of the keys' tokens)
   const double behind = n_rows < P.key_tiles * PW_KEYS ? static_cast<double>(n_rows) / (P.key_tiles * PW_KEYS) : 1.0;
   const double share = seen < P.key_tiles ? static_cast<double>(seen) / P.key_tiles : 1.0 - 0.5 * behind;
-  const PwPlan plan = pw_plan(d.d_head, d.n_kv_heads, group, n_rows, P.key_tiles, seen < P.key_tiles ? seen : P.key_tiles, share);
+  const PwPlan plan = pw_plan(d.d_head, d.n_kv_heads, group, n_rows, P.key_tiles, seen, share);
   P.ranges = (plan.row_tiles + plan.range - 1) / plan.range;
   const size_t ml_bytes = pw_ml_bytes(d.n_kv_heads, plan.row_tiles, plan.splits);
   if (ml_bytes + static_cast<size_t>(P.ranges) * d.n_kv_heads * P.key_tiles * PW_KEYS * sizeof(float) > scratch_bytes) return KVD_ERR_CAPACITY;

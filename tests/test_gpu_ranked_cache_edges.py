@@ -130,3 +130,23 @@ def test_evict_refuses_rows_that_do_overlap():
     no((kv, other, None, w, 2 * row, 64), (kv[:, :, row - 8:], torch.zeros_like(kv), None, None, 2 * row, 64))
     no((kv, other, None, w, row, 64), (kv[:, 32:], torch.zeros_like(kv), None, None, 2 * row, 64))  # other strides over the same rows
     assert ctx.kvd_launch_count() == launches
+
+
+# ------------------------------------------------------------------------------------------------ a window without an end
+@pytest.mark.parametrize("shape,rows,ctx_len", [("gemma", 64, 3000), ("smollm2", 300, 0), ("qwen", 700, 1500)])
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 40, 2**30])
+def test_prompt_weights_of_a_window_that_hides_nothing(shape, rows, ctx_len, window):
+    """Windows up to the largest that a layer can have: cut into the launches of a layer without one, hence its bits."""
+    nq, nkv, dh = SHAPES[shape]
+    g, t = gen(rows), rows + ctx_len
+    k, q = rnd(g, t, nkv, dh), rnd(g, rows, nq, dh)
+    pos = torch.arange(ctx_len, t, dtype=torch.int32, device="cuda")
+    got = []
+    for w in (0, window):
+        ctx, desc = open_ctx(shape, 0, w)
+        scratch = torch.empty(kvd.kvd_prefill_weights_scratch_bytes(desc, rows, t), dtype=torch.uint8, device="cuda")
+        got.append(torch.empty(t, device="cuda"))
+        ctx.kvd_prefill_attention_weights(0, rows, q, pos, [(k, None, nkv * dh, 0, t)], 0.0, None, got[-1], t, scratch)
+        assert ctx.kvd_poll_status() == kvd.KVD_OK
+    assert abs(float(got[0].double().sum()) - rows * nq) < 1e-4 * rows * nq
+    assert torch.equal(got[0], got[1])
