@@ -397,10 +397,9 @@ kvd_status kvd_prefill_attention(kvd_ctx *ctx, int layer, int n_rows, const void
  * sequence's own in the merge.  prefix->len == 0 is kvd_decode_attention.  The split of the prefix depends on the batch and
  * its weights are rounded to the element type before the second product, so the bits are not those of kvd_decode_attention
  * (same tolerance against the definition), and a sequence's bits may depend on the batch's size.  The prefix must not
- * overlap a sequence's own segments in position.  Where sequences see the prefix in part (a sliding window, a query inside
- * it), a value that is not finite reaches the sequences that do not see it as well (0 times infinity), if they see another
- * key of its block of 128 (64 at d_head 256).  n_segs <= KVD_MAX_SEGMENTS.  bf16 and fp16 contexts; needs an attached
- * workspace. */
+ * overlap a sequence's own segments in position.  Keys and values of the prefix that are not finite concern the sequences that
+ * see them alone (a sequence whose share of a block is partly hidden and holds such a value is attended again, more slowly).
+ * n_segs <= KVD_MAX_SEGMENTS.  bf16 and fp16 contexts; needs an attached workspace. */
 kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int batch, const void *q, const int32_t *q_pos,
                                        const kvd_kv_segment *prefix, const kvd_kv_segment *segs, int n_segs, float scale,
                                        void *out, void *stream);

@@ -1097,6 +1097,10 @@ extern "C" kvd_status kvd_shared_prefix_attention(kvd_ctx *ctx, int layer, int b
       if (pass == 0) continue;
       if (P.splits > 0) {
         P.q = L.q;
+        P.k = static_cast<const __nv_bfloat16 *>(prefix->k);
+        P.v = static_cast<const __nv_bfloat16 *>(prefix->v);
+        P.stride = prefix->row_stride;
+        P.len = prefix->len;
         P.n_q = d.n_q_heads;
         P.n_kv = d.n_kv_heads;
         P.scale_log2e = L.scale_log2e;

@@ -440,6 +440,9 @@ kvd_status launch_checkpoint_scatter(kvd_ctx *ctx, const __nv_bfloat16 *rows, co
 // kvd_shared_prefix_attention: the partials of a launch's sequences over the prefix they share
 struct SharedPrefixParams {
   const __nv_bfloat16 *q;  // [sequences][n_q][d_head] (already offset to the launch's first sequence)
+  const __nv_bfloat16 *k, *v;  // the prefix (what the tensor maps describe)
+  long long stride;
+  int len;
   int n_q, n_kv;
   float scale_log2e;
   int seqs, row_tiles;     // tiles of 128 (sequence, head of the group) pairs of a KV head

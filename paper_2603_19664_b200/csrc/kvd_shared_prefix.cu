@@ -24,6 +24,8 @@
 #include <math_constants.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "kvd_internal.h"
 #include "kvd_ptx.cuh"
 
@@ -73,6 +75,49 @@ struct SpMaps {
   CUtensorMap q;     // [sequences][n_q][d_head], boxes of 64 channels, a group's heads and a tile's sequences
   CUtensorMap k, v;  // [len][n_kv * d_head], boxes of 64 channels and a block's keys
 };
+
+// The unnormalised output of one row (its first query value at q) over the keys a .. b of the prefix that it sees, in fp32, by a warp:
+// a lane has D_HEAD / 32 channels.  For rows whose tile has met a value that is not finite (below).
+template <int D_HEAD, int DT>
+__device__ __noinline__ void sp_redo_row(const SharedPrefixParams &P, const __nv_bfloat16 *q, int kvh, int a, int b, float mu, float *out, int lane) {
+  constexpr int W = D_HEAD / 64;  // words of a lane's channels
+  typedef typename std::conditional<W == 1, uint32_t, typename std::conditional<W == 2, uint2, uint4>::type>::type Words;
+  union Piece {
+    Words all;
+    uint32_t w[W];
+  };
+  const long long first = static_cast<long long>(kvh) * D_HEAD + lane * 2 * W;
+  Piece piece;
+  uint64_t x[W], o[W];
+  piece.all = *reinterpret_cast<const Words *>(q + lane * 2 * W);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    x[i] = x2_to_f32x2<DT>(piece.w[i]);
+    o[i] = 0ull;
+  }
+#pragma unroll 1
+  for (int j = a; j <= b; ++j) {
+    piece.all = *reinterpret_cast<const Words *>(P.k + j * P.stride + first);
+    uint64_t dot = 0ull;
+#pragma unroll
+    for (int i = 0; i < W; ++i) dot = ffma2(x2_to_f32x2<DT>(piece.w[i]), x[i], dot);
+    float s0, s1;
+    unpack2(dot, s0, s1);
+    s0 += s1;
+#pragma unroll
+    for (int i = 16; i >= 1; i >>= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, i);
+    const float p = ex2_approx(fmaf(s0, P.scale_log2e, -mu));
+    piece.all = *reinterpret_cast<const Words *>(P.v + j * P.stride + first);
+#pragma unroll
+    for (int i = 0; i < W; ++i) o[i] = ffma2(pack2(p, p), x2_to_f32x2<DT>(piece.w[i]), o[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    float2 f;
+    unpack2(o[i], f.x, f.y);
+    reinterpret_cast<float2 *>(out + lane * 2 * W)[i] = f;
+  }
+}
 
 template <int D_HEAD, int G, int DT, int NT>
 __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
@@ -231,11 +276,21 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
       const long long slot = valid ? static_cast<long long>(P.slot[seq]) + split : 0;
       const bool store = valid && KVD_BOUNDS_OK(slot >= 0 && slot < P.max_parts, P.status);
       const long long at = slot * P.n_q + head;
+      // A product takes in all keys of a block, those that a row does not see with weight 0: a value there that is not finite makes
+      // the row's output a NaN (0 times infinity).  Rows that see less than the CTA's keys are looked through for it, and taken
+      // again over the keys that they see.
+      const int last = min(key0 + n_blk * BK, P.len) - 1;
+      const bool in_part = valid && (lo > key0 || hi < last);
+      bool odd = false;
 #pragma unroll 1
       for (int c = 0; c < D_HEAD / 32; ++c) {
         uint32_t r[32];
         tmem_ld_x32(tmem_base + lane_field + Cfg::COL_O + t * D_HEAD + c * 32, r);
         tmem_wait_ld();
+        if (in_part) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) odd |= (r[i] & 0x7f800000u) == 0x7f800000u;
+        }
         if (store) {
           // (32 bytes at a time: whole sectors, whose halves would be written one by one otherwise)
           store_row_piece<8>(reinterpret_cast<__nv_bfloat16 *>(P.part_o + at * D_HEAD + c * 32), r, true);
@@ -245,6 +300,16 @@ __global__ void __launch_bounds__(SpCfg<D_HEAD, NT>::THREADS, 1)
       unpack2(l2[0], a0, a1);
       unpack2(l2[1], a2, a3);
       if (store) *reinterpret_cast<float2 *>(P.part_ml + at * 2) = make_float2(m, (a0 + a1) + (a2 + a3));
+      __syncwarp();
+      for (uint32_t rows = __ballot_sync(0xffffffffu, odd && store); rows != 0u; rows &= rows - 1u) {
+        const int of = __ffs(static_cast<int>(rows)) - 1;
+        const int seq_of = __shfl_sync(0xffffffffu, seq, of), head_of = __shfl_sync(0xffffffffu, head, of);
+        const float m_of = __shfl_sync(0xffffffffu, m, of);
+        const int a = max(key0, __shfl_sync(0xffffffffu, lo, of)), b = min(last, __shfl_sync(0xffffffffu, hi, of));
+        const long long at_of = __shfl_sync(0xffffffffu, at, of);
+        sp_redo_row<D_HEAD, DT>(P, P.q + (static_cast<long long>(seq_of) * P.n_q + head_of) * D_HEAD, kvh, a, b, m_of == -CUDART_INF_F ? 0.f : m_of,
+                                P.part_o + at_of * D_HEAD, lane);
+      }
     }
   } else if (warp == 4 * NT) {
     // ------------------------------------------------------------------ products (one thread)

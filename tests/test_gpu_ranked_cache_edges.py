@@ -150,3 +150,54 @@ def test_prompt_weights_of_a_window_that_hides_nothing(shape, rows, ctx_len, win
         assert ctx.kvd_poll_status() == kvd.KVD_OK
     assert abs(float(got[0].double().sum()) - rows * nq) < 1e-4 * rows * nq
     assert torch.equal(got[0], got[1])
+
+
+# ------------------------------------------------------------------------------------------------ a prefix with values that are no numbers
+@pytest.mark.parametrize("shape,dtype,copies,own", [("smollm2", 0, 1, 0), ("smollm2", 1, 6, 3), ("gemma", 0, 1, 1), ("gemma", 1, 3, 200), ("qwen", 0, 1, 2),
+                                                    ("qwen", 1, 5, 200), ("g8-256", 0, 1, 90)])
+@pytest.mark.parametrize("window", [0, 333])
+def test_shared_prefix_with_values_that_are_not_finite(shape, dtype, copies, own, window):
+    """A value of the prefix that is not finite, or a key, concerns the sequences that see it and nobody else: not those before
+    it, those whose window has moved on, nor those that see other keys of the same block."""
+    nq, nkv, dh = SHAPES[shape]
+    prefix, first = 1500, 20
+    q_pos = [19, 25, 700, 1395, 1399, 1400, 1519, 1600, 1732, 1733, 1740, 1853, 1900] * copies
+    b, end = len(q_pos), first + prefix
+    ctx, _ = open_ctx(shape, dtype, window, max_batch=b)
+    g, row, dt = gen(53), nkv * dh, DT[dtype]
+    pk, pv = rnd(g, prefix, nkv, dh, dtype=dt, std=0.5), rnd(g, prefix, nkv, dh, dtype=dt)
+    k, v, q = rnd(g, b, 512, nkv, dh, dtype=dt, std=0.5), rnd(g, b, 512, nkv, dh, dtype=dt), rnd(g, b, nq, dh, dtype=dt)
+    # own keys end at the query's token (or lie ahead of the prefix's tokens that the query does not see)
+    own_at = [(max(end, p + 1 - own), p + 1) for p in q_pos]
+    segs = [[(k[i], v[i], row, lo, hi - lo)] if hi > lo and own else [] for i, (lo, hi) in enumerate(own_at)]
+    out = torch.empty_like(q)
+    bad = 1400 - first
+    for what in ("values", "keys"):
+        pk2, pv2 = pk.clone(), pv.clone()
+        if what == "values":
+            pv2[bad, 0, 3], pv2[bad, nkv - 1, dh - 1] = math.inf, math.nan
+        else:
+            pk2[bad, 0, :2], pk2[bad, nkv - 1, 1] = math.inf, math.nan
+        ctx.kvd_shared_prefix_attention(0, b, q, q_pos, (pk2, pv2, row, first, prefix), segs, 0.0, out)
+        assert ctx.kvd_poll_status() == kvd.KVD_OK
+        for i, p in enumerate(q_pos):
+            at = torch.arange(first, end, device="cuda")
+            n = own_at[i][1] - own_at[i][0] if segs[i] else 0
+            seen = at <= p
+            mine = torch.arange(own_at[i][0], own_at[i][0] + n, device="cuda")
+            if window:
+                seen, ours = seen & (at > p - window), mine > p - window
+            else:
+                ours = torch.ones(n, dtype=torch.bool, device="cuda")
+            if bool(seen[bad]):
+                if what == "values":  # in its channel of its KV head's queries, and there alone
+                    group = nq // nkv
+                    assert not bool(torch.isfinite(out[i, :group, 3]).any()) and not bool(torch.isfinite(out[i, nq - group:, dh - 1]).any())
+                    assert int((~torch.isfinite(out[i])).sum()) == 2 * group
+                continue
+            seen = torch.cat([seen, ours])
+            if not bool(seen.any()):
+                assert not bool(out[i].any())
+                continue
+            p64 = softmax64(q[i], torch.cat([pk, k[i, :n]]), 1 / math.sqrt(dh), seen)
+            close(out[i], out64(p64, torch.cat([pv, v[i, :n]])), O_TOL)
