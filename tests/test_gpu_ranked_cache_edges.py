@@ -201,3 +201,52 @@ def test_shared_prefix_with_values_that_are_not_finite(shape, dtype, copies, own
                 continue
             p64 = softmax64(q[i], torch.cat([pk, k[i, :n]]), 1 / math.sqrt(dh), seen)
             close(out[i], out64(p64, torch.cat([pv, v[i, :n]])), O_TOL)
+
+
+# ------------------------------------------------------------------------------------------------ several own segments behind a prefix
+@pytest.mark.parametrize("shape,dtype", [("smollm2", 0), ("gemma", 0), ("gemma", 1), ("qwen", 0), ("qwen", 1), ("g1", 0), ("g8", 0), ("g8-256", 0)])
+@pytest.mark.parametrize("window", [0, 250])
+@pytest.mark.parametrize("copies", [1, 8])
+def test_shared_prefix_ahead_of_several_own_segments(shape, dtype, window, copies):
+    """Rebuilt keys, a window and the current token behind the prefix, as a bounded cache has them: with holes, segments of one
+    key, keys ahead of the prefix, empty segments, and sequences whose live keys are a handful."""
+    nq, nkv, dh = SHAPES[shape]
+    prefix, first = 700, 50
+    end = first + prefix
+    cuts = [[(end, end + 300), (end + 300, end + 420), (end + 420, end + 421)], [(end, end + 1)], [(end + 3, end + 4), (end + 9, end + 10)],
+            [(0, 40), (end, end + 130), (end + 200, end + 201), (end + 201, end + 202)], [], [(10, 50), (end + 100, end + 100), (end + 120, end + 128)],
+            [(end, end + 64), (end + 70, end + 90)]]
+    q_pos = [end + 420, end, end + 9, end + 201, end + 5, end + 127, end + 95]
+    cuts, q_pos = cuts * copies, q_pos * copies
+    b, cap = len(cuts), end + 500
+    ctx, _ = open_ctx(shape, dtype, window, max_batch=b)
+    g, row, dt = gen(61), nkv * dh, DT[dtype]
+    pk, pv = rnd(g, prefix, nkv, dh, dtype=dt), rnd(g, prefix, nkv, dh, dtype=dt)
+    k, v, q = rnd(g, b, cap, nkv, dh, dtype=dt), rnd(g, b, cap, nkv, dh, dtype=dt), rnd(g, b, nq, dh, dtype=dt)
+    pos = torch.arange(cap, device="cuda")
+    seen = torch.zeros((b, cap), dtype=torch.bool, device="cuda")
+    for i, c in enumerate(cuts):
+        seen[i, first:end] = True
+        for lo, hi in c:
+            seen[i, lo:hi] = True
+        seen[i] &= pos <= q_pos[i]
+        if window:
+            seen[i] &= pos > q_pos[i] - window
+    # own rows that nobody sees are not numbers
+    k[~seen], v[~seen] = math.nan, math.inf
+    segs = [segments(k[i], v[i], c, row) for i, c in enumerate(cuts)]
+    out, joint = torch.empty_like(q), torch.empty_like(q)
+    ctx.kvd_shared_prefix_attention(0, b, q, q_pos, (pk, pv, row, first, prefix), segs, 0.0, out)
+    assert ctx.kvd_poll_status() == kvd.KVD_OK
+    for i in range(b):
+        kk, vv = k[i].clone(), v[i].clone()
+        kk[first:end], vv[first:end] = pk, pv
+        kk = torch.where(seen[i][:, None, None], kk, torch.zeros((), dtype=dt, device="cuda"))
+        vv = torch.where(seen[i][:, None, None], vv, torch.zeros((), dtype=dt, device="cuda"))
+        close(out[i], out64(softmax64(q[i], kk, 1 / math.sqrt(dh), seen[i]), vv), O_TOL)
+    # the prefix listed among the segments of a call of its own, where there is room for it
+    few = [i for i, c in enumerate(cuts) if len(c) < B.KVD_MAX_SEGMENTS][:7]
+    ctx.kvd_decode_attention(0, len(few), q[few].contiguous(), [q_pos[i] for i in few], [[(pk, pv, row, first, prefix)] + segs[i] for i in few], 0.0, joint)
+    assert ctx.kvd_poll_status() == kvd.KVD_OK
+    for n, i in enumerate(few):
+        close(out[i], joint[n].double(), 2 * O_TOL)
