@@ -58,8 +58,9 @@ struct EvictParams {
   int len[EV_MAX_SEQS], protect_from[EV_MAX_SEQS];
 };
 
+// (words: a single CTA's holes, at most half of its slots, follow its counts in hist; a small cache's places the unused ones in sum)
 static_assert(3 * EV_BINS >= EV_SMALL, "places of a small cache");
-static_assert(12 * EV_BINS >= EV_RUN, "a single CTA's holes: at most half of its slots");
+static_assert(2 * 3 * EV_BINS >= EV_RUN, "a single CTA's holes");
 struct EvictShared {
   uint32_t hist[3][EV_BINS];    // this CTA's counts, by pass; a single CTA's holes after that
   uint32_t sum[3][EV_BINS];     // rank 0: the cluster's, added up by remote atomics

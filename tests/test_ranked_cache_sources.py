@@ -2,8 +2,6 @@
 import os
 import re
 
-import pytest  # noqa: F401
-
 from test_ranked_cache_rules import CSRC, KERNELS
 
 
@@ -31,3 +29,22 @@ def test_no_weight_is_read_once_a_cta_of_the_cluster_may_write_it():
         assert barrier in text[read:]
     # (a barrier that only some CTAs reached would hang: the branch hangs on T alone, which all of them find from the same keys)
     assert "rank" not in again and "copy " not in again
+
+
+def test_the_selections_lists_fit_the_counts_they_follow():
+    """A single CTA's holes (half of its slots at most) lie where its counts were, a small cache's places behind them where the
+    cluster's were: a size that breaks either does not compile."""
+    text = open(os.path.join(CSRC, "kvd_evict.cu")).read()
+    struct = _block(text, text.index("struct EvictShared"))
+    assert "hist[3][EV_BINS];" in struct and "sum[3][EV_BINS];" in struct and struct.index("hist[3]") < struct.index("sum[3]")
+    body = KERNELS["kvd_evict_select_kernel"][1]
+    assert re.search(r"\*holes = &S\.hist\[0\]\[0\], \*source = &S\.sum\[0\]\[0\]", body)
+    consts = {m.group(1): int(eval(m.group(2))) for m in re.finditer(r"constexpr int (EV_\w+) = ([0-9 <]+);", text)}
+    claims = re.findall(r"static_assert\(([^\"]*), \"", text)
+
+    def compiles(**changed):
+        return all(eval(c, {}, {**consts, **changed}) for c in claims)
+
+    words = 3 * consts["EV_BINS"]
+    assert compiles() and compiles(EV_RUN=2 * words) and compiles(EV_SMALL=words)
+    assert not compiles(EV_RUN=2 * words + 2) and not compiles(EV_SMALL=words + 1)
