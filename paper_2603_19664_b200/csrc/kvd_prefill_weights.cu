@@ -56,6 +56,7 @@ struct PwParams {
   float2 *ml;              // [splits][n_kv][row_tiles * 128]: reference and sum of a row's share; (-inf, 0): nothing seen
   int key_tile0, key_tiles, chunk, chunks, range, ranges;  // columns pass: key tiles per CTA, row tiles per CTA
   float *cols;             // [ranges][n_kv][key_tiles * 128]
+  long long ml_size, cols_size;  // elements the scratch has room for (checking build)
   const float *in;
   float *out;
   int n_positions;
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
         t += a;
         n = b - a;
       }
-      if (lane == 0) {
+      if (lane == 0 && KVD_BOUNDS_OK(i < PW_RANGE, P.status)) {
         s_tile[i] = t;
         s_count[i] = n;
         s_qmin[i] = qmin;
@@ -428,7 +429,9 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
         for (int s0 = share; s0 < P.splits; s0 += 4 * PER) {
           float2 v[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = s0 + PER * u < P.splits ? __ldcg(src + (s0 + PER * u) * n) : make_float2(-CUDART_INF_F, 0.f);
+          for (int u = 0; u < 4; ++u)
+            v[u] = s0 + PER * u < P.splits && KVD_BOUNDS_OK(src + (s0 + PER * u) * n < P.ml + P.ml_size, P.status) ? __ldcg(src + (s0 + PER * u) * n)
+                                                                                                                   : make_float2(-CUDART_INF_F, 0.f);
           const float mn = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x))), mu = mn == -CUDART_INF_F ? 0.f : mn;
           l *= ex2_approx(m - mu);
 #pragma unroll
@@ -544,7 +547,8 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
           float a0, a1, a2, a3;
           unpack2(acc[0], a0, a1);
           unpack2(acc[1], a2, a3);
-          s_sum[grp][(t0 + jj - kt_lo) * PW_KEYS + row] += (a0 + a1) + (a2 + a3);
+          if (KVD_BOUNDS_OK(t0 + jj >= kt_lo && t0 + jj < kt_lo + PW_CHUNK, P.status))
+            s_sum[grp][(t0 + jj - kt_lo) * PW_KEYS + row] += (a0 + a1) + (a2 + a3);
         }
         j0 += n_blk;
         ++nth;
@@ -657,8 +661,10 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
   }
   if constexpr (COLUMNS) {
     // (also the sums of a CTA that gave up: the status word says so)
-    float *dst = P.cols + (static_cast<long long>(part) * P.n_kv + kvh) * P.key_tiles * PW_KEYS + (kt_lo - P.key_tile0) * PW_KEYS;
+    const long long first = (static_cast<long long>(part) * P.n_kv + kvh) * P.key_tiles * PW_KEYS + (kt_lo - P.key_tile0) * PW_KEYS;
+    float *dst = P.cols + first;
     for (int i = tid; i < (kt_hi - kt_lo) * PW_KEYS; i += Cfg::THREADS) {
+      if (!KVD_BOUNDS_OK(i < PW_CHUNK * PW_KEYS && first + i < P.cols_size, P.status)) break;
       float w = 0.f;
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g) w += s_sum[g][i];
@@ -672,7 +678,8 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) l = fmaf(ex2_approx(s_ml[g][tid].x - mu), s_ml[g][tid].y, l);
     const bool there = tid < TOK * G && tile0 * TOK + tid / G < P.n_rows;
-    P.ml[((static_cast<long long>(part) * P.n_kv + kvh) * P.row_tiles + tile0) * PW_ROWS + tid] = there ? make_float2(m, l) : make_float2(-CUDART_INF_F, 0.f);
+    const long long at = ((static_cast<long long>(part) * P.n_kv + kvh) * P.row_tiles + tile0) * PW_ROWS + tid;
+    if (KVD_BOUNDS_OK(at < P.ml_size, P.status)) P.ml[at] = there ? make_float2(m, l) : make_float2(-CUDART_INF_F, 0.f);
   }
 }
 
@@ -688,7 +695,7 @@ __global__ void __launch_bounds__(PW_SUM * 32) kvd_prefill_weights_sum_kernel(co
   float sum = 0.f;
   if (p < P.n_positions && col >= 0 && col < width) {
 #pragma unroll 8
-    for (int i = warp; i < n; i += warps) sum += __ldcg(P.cols + i * width + col);
+    for (int i = warp; i < n; i += warps) sum += KVD_BOUNDS_OK(i * width + col < P.cols_size, P.status) ? __ldcg(P.cols + i * width + col) : 0.f;
   }
   s_part[warp][lane] = sum;
   __syncthreads();
@@ -882,6 +889,8 @@ extern "C" kvd_status kvd_prefill_attention_weights(kvd_ctx *ctx, int layer, int
   if (ml_bytes + static_cast<size_t>(P.ranges) * d.n_kv_heads * P.key_tiles * PW_KEYS * sizeof(float) > scratch_bytes) return KVD_ERR_CAPACITY;
   P.ml = static_cast<float2 *>(scratch);
   P.cols = reinterpret_cast<float *>(static_cast<uint8_t *>(scratch) + ml_bytes);
+  P.ml_size = static_cast<long long>(ml_bytes / sizeof(float2));
+  P.cols_size = static_cast<long long>((scratch_bytes - ml_bytes) / sizeof(float));
   static thread_local PwMaps M;
   {
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d.d_head), static_cast<cuuint64_t>(d.n_q_heads), static_cast<cuuint64_t>(n_rows)};

@@ -250,3 +250,17 @@ def test_shared_prefix_ahead_of_several_own_segments(shape, dtype, window, copie
     assert ctx.kvd_poll_status() == kvd.KVD_OK
     for n, i in enumerate(few):
         close(out[i], joint[n].double(), 2 * O_TOL)
+
+
+def test_indices_of_the_prompt_weights_hold_in_the_checking_build():
+    """Their kernels test what they index (statistics, sums, partial columns) at several cuts of the work."""
+    import os
+    import subprocess
+    import sys
+    if os.environ.get("KVD_LIBRARY") == "check":
+        pytest.skip("already the checking build")
+    here = os.path.dirname(os.path.abspath(__file__))
+    run = subprocess.run([sys.executable, "-m", "pytest", "-q", "-x", "-m", "gpu", os.path.join(here, "test_gpu_ranked_cache.py"), os.path.abspath(__file__),
+                          "-k", "test_prompt_weights and not refusals"], env=dict(os.environ, KVD_LIBRARY="check"), cwd=os.path.dirname(here),
+                         capture_output=True, text=True, timeout=600)
+    assert run.returncode == 0 and " passed" in run.stdout, run.stdout[-2000:] + run.stderr[-1000:]

@@ -2,6 +2,8 @@
 import os
 import re
 
+import pytest
+
 from test_ranked_cache_rules import CSRC, KERNELS
 
 
@@ -48,3 +50,20 @@ def test_the_selections_lists_fit_the_counts_they_follow():
     words = 3 * consts["EV_BINS"]
     assert compiles() and compiles(EV_RUN=2 * words) and compiles(EV_SMALL=words)
     assert not compiles(EV_RUN=2 * words + 2) and not compiles(EV_SMALL=words + 1)
+
+
+@pytest.mark.parametrize("kernel,accesses", [
+    ("kvd_prefill_weights_kernel", [r"P\.ml\[at\]", r"__ldcg\(src \+", r"s_sum\[grp\]\[[^;]*\] \+=", r"\bdst\[i\] = ", r"\bs_tile\[i\] = "]),
+    ("kvd_prefill_weights_sum_kernel", [r"__ldcg\(P\.cols \+"]),
+])
+def test_the_checking_build_tests_what_the_prompt_weights_kernels_index(kernel, accesses):
+    """Row tiles, statistics, sums in shared memory and partial columns: every index derived on the device stands behind a test."""
+    body = KERNELS[kernel][1]
+    for access in accesses:
+        found = list(re.finditer(access, body))
+        assert found, access
+        for m in found:  # in the access's line, or in the few ahead of it
+            lines = body[:m.start()].split("\n")[-6:]
+            assert any("KVD_BOUNDS_OK(" in line for line in lines), body[m.start():m.end()]
+    # every such access is one of those
+    assert not re.search(r"P\.ml\[\(|P\.cols\[", body)
