@@ -566,6 +566,10 @@ kvd_status kvd_poll_status(kvd_ctx *ctx, void *stream);
  * stays usable. */
 kvd_status kvd_selftest_wait_timeout(kvd_ctx *ctx, int limit_ms, void *stream);
 
+/* Self-test of the exponential that kvd_prefill_attention_weights takes on the fp32 pipes for part of its scores: out[i] =
+ * 2^in[i] (DEVICE fp32, 8-byte aligned, n even).  upper = 0: the form for arguments up to 0 (any below about 127), 1: for any. */
+kvd_status kvd_selftest_exp2(kvd_ctx *ctx, const float *in, float *out, int n, int upper, void *stream);
+
 /* The checking build (libkvd_check.so: the same sources compiled with -DKVD_CHECK; python -m
  * paper_2603_19664_b200.build --check).  Its kernels test the indices they derive on the device -- the job and
  * row block a tile belongs to, the rows of a store range, the slot of a residual row, the slot of an attention

@@ -43,7 +43,7 @@ EXPORTED_SYMBOLS = (
     "kvd_checkpoint_residual_fp4", "kvd_fp4_scratch_bytes", "kvd_recompute_kv_fp4",
     "kvd_rows_stored", "kvd_workspace_bytes", "kvd_attention_split", "kvd_attach_workspace", "kvd_checkpoint_residual", "kvd_checkpoint_residual_step", "kvd_decode_step_kv", "kvd_recompute_kv",
     "kvd_recompute_kv_step",
-    "kvd_decode_attention", "kvd_decode_attention_rows", "kvd_prefill_attention", "kvd_decode_attention_static", "kvd_memory_stats", "kvd_poll_status", "kvd_selftest_wait_timeout", "kvd_build_has_checks", "kvd_selftest_bounds_check", "kvd_set_trace", "kvd_trace_bytes", "kvd_launch_count", "kvd_last_cuda_error",
+    "kvd_decode_attention", "kvd_decode_attention_rows", "kvd_prefill_attention", "kvd_decode_attention_static", "kvd_memory_stats", "kvd_poll_status", "kvd_selftest_wait_timeout", "kvd_selftest_exp2", "kvd_build_has_checks", "kvd_selftest_bounds_check", "kvd_set_trace", "kvd_trace_bytes", "kvd_launch_count", "kvd_last_cuda_error",
     "kvd_status_string", "kvd_version",
     "kvd_shared_prefix_attention", "kvd_weights_scratch_bytes", "kvd_decode_attention_weights", "kvd_prefill_weights_scratch_bytes",
     "kvd_prefill_attention_weights", "kvd_cache_evict",
@@ -248,6 +248,8 @@ def load() -> ctypes.CDLL:
     lib.kvd_poll_status.restype = i32
     lib.kvd_selftest_wait_timeout.argtypes = [vp, i32, vp]
     lib.kvd_selftest_wait_timeout.restype = i32
+    lib.kvd_selftest_exp2.argtypes = [vp, vp, vp, i32, i32, vp]
+    lib.kvd_selftest_exp2.restype = i32
     lib.kvd_build_has_checks.argtypes = []
     lib.kvd_build_has_checks.restype = i32
     lib.kvd_selftest_bounds_check.argtypes = [vp, vp]
@@ -769,6 +771,10 @@ class Kvd:
     def kvd_selftest_wait_timeout(self, limit_ms: int, stream=None) -> None:
         self._check(self._lib.kvd_selftest_wait_timeout(self._h, limit_ms, _stream(stream)),
                     "kvd_selftest_wait_timeout")
+
+    def kvd_selftest_exp2(self, values, out, upper: bool, stream=None) -> None:
+        """2^values by the fp32 pipes' exponential; values, out: float32 device tensors of an even number of elements."""
+        self._check(self._lib.kvd_selftest_exp2(self._h, _ptr(values), _ptr(out), values.numel(), int(upper), _stream(stream)), "kvd_selftest_exp2")
 
     def kvd_selftest_bounds_check(self, stream=None) -> int:
         """Returns the status (KVD_ERR_UNSUPPORTED in the release build) instead of raising."""

@@ -197,9 +197,10 @@ __device__ __forceinline__ uint64_t pw_ex2(uint64_t e) {
   return pack2(ex2_approx(e0), ex2_approx(e1));
 }
 // The same on the fp32 pipes: e = n + f with n whole and |f| <= 1/2 (adding and taking away 1.5 * 2^23 rounds to whole numbers),
-// 2^f by the polynomial of degree 5 that is nearest to it in relative error over [-1/2, 1/2] (2e-7 with its coefficients and steps
-// in fp32, like ex2.approx), n added to the exponent.  Below 2^-127: exactly 0.  UPPER: also for e that may be large -- the
-// result is then at least 2^127; a NaN gives more than 1e30 or a NaN, and so does plus infinity.
+// 2^f by a polynomial of degree 5 with the constant term 1, n added to the exponent.  Over [-1/2, 1/2] the polynomial is off by
+// -1.6e-7 to 1.5e-8 of the value (the degree's least error, to either side, with its constant term rounded to 1), with the steps'
+// roundings by 2.5e-7 at most; ex2.approx by 2.4e-7.  From -126 down results lose bits, at and below -127 they are exactly 0.  UPPER:
+// also for e that may be large -- the result is then at least 2^127; a NaN gives more than 1e30 or a NaN, and so does plus infinity.
 template <bool UPPER>
 __device__ __forceinline__ uint64_t pw_ex2_poly(uint64_t e) {
   float e0, e1, t0, t1, p0, p1;
@@ -683,6 +684,16 @@ __global__ void __launch_bounds__(PwCfg<D_HEAD, COLUMNS>::THREADS, PwCfg<D_HEAD,
   }
 }
 
+// The exponential on the fp32 pipes by itself (kvd_selftest_exp2), a pair per thread.
+template <bool UPPER>
+__global__ void kvd_selftest_exp2_kernel(const float2 *in, float2 *out, int pairs) {
+  const int i = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x);
+  if (i >= pairs) return;
+  float2 v = in[i];
+  unpack2(pw_ex2_poly<UPPER>(pack2(v.x, v.y)), v.x, v.y);
+  out[i] = v;
+}
+
 // out_p = in_p + the partial columns of position p: 32 positions per CTA, PW_SUM warps over the partials, added in order.
 constexpr int PW_SUM = 32;
 __global__ void __launch_bounds__(PW_SUM * 32) kvd_prefill_weights_sum_kernel(const __grid_constant__ PwParams P) {
@@ -807,6 +818,19 @@ static kvd_status pw_group(kvd_ctx *ctx, const PwParams &P, const PwMaps &M, int
 }  // namespace kvd
 
 using namespace kvd;
+
+extern "C" kvd_status kvd_selftest_exp2(kvd_ctx *ctx, const float *in, float *out, int n, int upper, void *stream) {
+  if (!ctx || n < 0 || n % 2 != 0) return KVD_ERR_INVALID_ARG;
+  if (n == 0) return KVD_OK;
+  if (!in || !out) return KVD_ERR_INVALID_ARG;
+  if (((reinterpret_cast<uintptr_t>(in) | reinterpret_cast<uintptr_t>(out)) & 7u) != 0) return KVD_ERR_ALIGNMENT;
+  const auto kern = upper ? kvd_selftest_exp2_kernel<true> : kvd_selftest_exp2_kernel<false>;
+  kern<<<(n / 2 + 255) / 256, 256, 0, static_cast<cudaStream_t>(stream)>>>(reinterpret_cast<const float2 *>(in), reinterpret_cast<float2 *>(out), n / 2);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "launch selftest_exp2");
+  ctx->launches += 1;
+  return KVD_OK;
+}
 
 extern "C" size_t kvd_prefill_weights_scratch_bytes(const kvd_model_desc *d, int n_rows, int n_positions) {
   if (kvd_workspace_bytes(d) == 0 || n_rows <= 0 || n_positions <= 0 || n_positions > (1 << 30)) return 0;  // (checks the description)

@@ -264,3 +264,51 @@ def test_indices_of_the_prompt_weights_hold_in_the_checking_build():
                           "-k", "test_prompt_weights and not refusals"], env=dict(os.environ, KVD_LIBRARY="check"), cwd=os.path.dirname(here),
                          capture_output=True, text=True, timeout=600)
     assert run.returncode == 0 and " passed" in run.stdout, run.stdout[-2000:] + run.stderr[-1000:]
+
+
+# ------------------------------------------------------------------------------------------------ the exponential on the fp32 pipes
+@pytest.mark.parametrize("upper", [False, True])
+def test_exponential_on_the_fp32_pipes(upper):
+    """Against 2^e in 64 bits.  From -126 to 127 the polynomial's 1.6e-7 (exact arithmetic, f = e - n is exact), the last step's
+    rounding, 2^-24 of a value in [1, 2) or 2^-25 of one above 0.7, and the half of 2^-25 that the step before it leaves: 2.5e-7.  Between
+    -127 and -126 results may lose their bits (2^-126), at and below -127 they are 0."""
+    ctx, _ = open_ctx("g1")
+    g = torch.Generator().manual_seed(71)
+    whole = torch.arange(-126, 127, dtype=torch.float64)
+    near = [0.0, 0.25, 0.5, 0.75] + [s * 2.0 ** -k for k in (3, 8, 12, 16, 20, 23) for s in (1, -1)] + [0.5 + s * 2.0 ** -k for k in (8, 12, 16, 20) for s in (1, -1)]
+    e = torch.cat([(whole[:, None] + torch.tensor(near, dtype=torch.float64)[None]).flatten(), torch.rand(200000, generator=g, dtype=torch.float64) * 253 - 126,
+                   torch.rand(100000, generator=g, dtype=torch.float64) * 2 - 1, -torch.exp(torch.rand(50000, generator=g, dtype=torch.float64) * 24 - 20)]).float()
+    e = e[(e >= -126) & (e <= (127 if upper else 126.5))]
+    inf, nan = math.inf, math.nan
+    low = torch.cat([-126 - torch.rand(2000, generator=g), torch.tensor([-126.5, -126.25, -126.75])])
+    low = low[(low > -127) & (low < -126)]
+    none = torch.tensor([-127.0, -127.5, -128.0, -150.0, -1000.0, -1e30, -3.4e38, -inf])
+    odd = torch.tensor([nan, -nan, inf] + ([127.0, 127.5, 128.0, 129.5, 1000.0, 1e30, 3.4e38] if upper else []))
+    x = torch.cat([e, low, none, odd])
+    x = torch.cat([x, x[:1]]) if x.numel() % 2 else x
+    for shift in (0, 1):  # either half of a pair
+        v = torch.roll(x, shift).cuda()
+        out = torch.full_like(v, -1.0)
+        ctx.kvd_selftest_exp2(v, out, upper)
+        got = torch.roll(out.cpu(), -shift).double()
+        a, b, c = e.numel(), e.numel() + low.numel(), e.numel() + low.numel() + none.numel()
+        want = torch.exp2(e.double())
+        off = ((got[:a] - want) / want).abs()
+        assert float(off.max()) <= 2.5e-7, (float(off.max()), float(e[off.argmax()]))
+        assert bool((got[a:b] >= 0).all()) and bool(((got[a:b] - torch.exp2(low.double())).abs() <= 2.0 ** -126).all())
+        assert not bool(got[b:c].any())
+        rest = got[c:c + odd.numel()]
+        assert not bool((rest <= 1e30).any())
+        if upper:
+            assert bool((rest[3:] >= 2.0 ** 127).all()) and float(rest[2]) >= 2.0 ** 127
+
+
+def test_exponential_refusals():
+    ctx, _ = open_ctx("g1")
+    x = torch.zeros(8, device="cuda")
+    out, launches = torch.full_like(x, 7.0), ctx.kvd_launch_count()
+    refused(B.KVD_ERR_INVALID_ARG, ctx.kvd_selftest_exp2, x[:3], out, False)
+    refused(B.KVD_ERR_INVALID_ARG, ctx.kvd_selftest_exp2, x, None, False)
+    refused(B.KVD_ERR_ALIGNMENT, ctx.kvd_selftest_exp2, x[1:7], out, False)
+    ctx.kvd_selftest_exp2(x[:0], out, False)
+    assert ctx.kvd_launch_count() == launches and bool((out == 7.0).all())
