@@ -867,9 +867,9 @@ __global__ void __launch_bounds__(AT_MERGE_THREADS)
 // position that the query does not see or that nobody holds keeps its weight; a head whose keys all score minus infinity
 // adds nothing.
 //
-// Bound by memory as the streaming kernel is: 16 x 8192 keys of a Qwen3-4B layer 113 us against 106 without weights, 17 MB of scores
-// written and read beside 520 MB of K and V; this launch 21 us, of which the merge alone takes most.  (A merge CTA per query
-// head: 122.)
+// 16 x 8192 keys of a Qwen3-4B layer: 115 us for the call, 106 without weights; 16 MB of scores are written and read beside
+// 519 MB of K and V (and 17 MB of partials either way).  This launch takes 23 alone, most of it the merge's, at a quarter of the
+// warps and 18 % of memory's rate.  (A merge CTA per query head: 122 for the call.)
 template <int NSEQ>
 __device__ __forceinline__ void attn_weigh_cta(const AttnLaunchT<NSEQ> &P, const AttnWeigh &W, int block) {
   extern __shared__ float at_merge_smem[];  // per head: -(m + log2 l), or minus infinity for a head that adds nothing
