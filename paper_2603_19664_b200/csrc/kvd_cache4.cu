@@ -401,6 +401,14 @@ __device__ __forceinline__ void lds_words(const uint8_t *p, uint32_t (&w)[W]) {
   }
 }
 
+// The weights' reference for a largest score: 12 below, or less, but not more (times a scale below 2, a weight of 2^15 is all that fp16 holds).  From
+// scores of 2^18 on, 12 below may round to something lower; no offset is taken then, and none from 2^27 on.
+__device__ __forceinline__ float c4_reference(float top) {
+  if (top == -INFINITY) return 0.f;
+  const float r = top - C4_OFFSET;
+  return top - r <= C4_OFFSET + 0x1p-6f ? r : top;
+}
+
 // A warp's sums over its chunk: lane (g, t) has heads 2 t, 2 t + 1.
 template <int DH>
 struct C4Sums {
@@ -494,7 +502,7 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
     tm0 = fmax3(tm0, s[x][0], s[x][2]);
     tm1 = fmax3(tm1, s[x][1], s[x][3]);
   }
-  if (__any_sync(0xffffffffu, tm0 > A.top0 + 3.0f || tm1 > A.top1 + 3.0f || (over & 0xffffu) > A.v_limit || (over >> 16) > A.v_limit)) {
+  if (__any_sync(0xffffffffu, tm0 - A.top0 > 3.0f || tm1 - A.top1 > 3.0f || (over & 0xffffu) > A.v_limit || (over >> 16) > A.v_limit)) {
     float n0 = tm0, n1 = tm1;
 #pragma unroll
     for (int d = 4; d < 32; d *= 2) {
@@ -521,7 +529,7 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
     }
     n0 = fmaxf(n0, A.top0);
     n1 = fmaxf(n1, A.top1);
-    const float r0 = n0 == -INFINITY ? 0.f : n0 - C4_OFFSET, r1 = n1 == -INFINITY ? 0.f : n1 - C4_OFFSET;
+    const float r0 = c4_reference(n0), r1 = c4_reference(n1);
     const float c0 = A.top0 == -INFINITY ? 0.f : ex2_approx(A.ref0 - r0), c1 = A.top1 == -INFINITY ? 0.f : ex2_approx(A.ref1 - r1);
     A.top0 = n0;
     A.top1 = n1;
@@ -602,7 +610,7 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
 //
 // Codes become fp16 exactly and are multiplied as they are: keys (16 x 16 channels a step) with the queries, and the scores of every
 // block of 32 channels with its scale in fp32; values, transposed by the way they are stored, with the softmax weights times
-// their token's scale.  The weights are 2^(s - m'), m' = the reference maximum less 12, and scales that are all below 2^-9, or some of
+// their token's scale.  The weights are 2^(s - m'), m' = the reference maximum less 12 (c4_reference), and scales that are all below 2^-9, or some of
 // them 2 or more, are taken a power of two times as large, so that fp16 rounds a weight and its product like any other down to
 // 2^-26 of the largest one.
 //
