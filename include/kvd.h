@@ -546,8 +546,11 @@ kvd_status kvd_cache4_expand(kvd_ctx *ctx, const kvd_paged_cache *cache, int lay
  * of sequence seqs[b] (HOST [batch], may repeat) and attends the keys and values that the cache holds of its lens[seqs[b]] = n tokens:
  * position p is seen iff p < n and, on a layer with a sliding window w, n - 1 - p < w or p < sinks (the first tokens that stay
  * visible; without a window `sinks` has no meaning).  Queries are read exactly, up to 2^-24 of the head's largest channel, sums
- * and statistics are fp32; the softmax weights are rounded to 11 bits twice on their way into the second product (below 2^-26 of the
- * largest one: to a multiple of 2^-36 of it; where scores are 2^18 or more, as powers of two, perhaps from 2^-14 on, to one of 2^-24).  What lies behind the
+ * and statistics are fp32; the softmax weights are rounded to 11 bits (below 2^-26 of the largest
+ * one: to a multiple of 2^-36 of it; where scores are 2^18 or more, as powers of two, perhaps from 2^-14 on, to one of 2^-24), and so are their
+ * products with a value's scale (a product below 2^-26 of the largest weight: to a multiple of 2^-36 of it, or of 2^-46 where no scale of the
+ * head is 2^-9 or more; where a scale of the block is 2 or more, both times the power of two at or below the block's largest).  In fp16 an output beyond
+ * 65504 becomes 65504.  What lies behind the
  * last token, in its page or its table, is never looked at.  A sequence without tokens yields zeros; values that are not finite
  * spread to the heads that see them.  How the keys are split follows from all lengths of the call, so a sequence's bits may depend
  * on its batch; equal calls give equal bits.  scale <= 0 selects 1/sqrt(d_head); out DEVICE [batch, n_q_heads, d_head], 16-byte

@@ -1,6 +1,8 @@
 // A cache held in 4 bits (kvd.h, kvd_pages.h): writing it, reading it back, and decode attention over it.
 #include <string.h>
 
+#include <type_traits>
+
 #include "kvd_internal.h"
 #include "kvd_pages.h"
 #include "kvd_ptx.cuh"
@@ -298,7 +300,8 @@ __global__ void __launch_bounds__(C4_ROW_THREADS) kvd_cache4_expand_kernel(const
 // ------------------------------------------------------------------------------------------------ decode attention
 constexpr int C4_SEQS = 64;             // sequences per launch
 constexpr int C4_MAX_CTAS = 320;        // of a launch: two for each of 160 SMs, more than any device of this kind has
-constexpr uint32_t C4_TINY = 0x17ff;    // fp16 bits of the largest number below 2^-9
+constexpr uint32_t C4_TINY = 0x17ff;    // fp16 bits of the largest number below 2^-9 ...
+constexpr uint32_t C4_USUAL = 0x3fff;   // ... and of that below 2
 constexpr float C4_OFFSET = 12.0f;
 constexpr int C4_RUN_COST = 28672;      // channels of a tile, over tiles
 constexpr int C4_AHEAD = 6;             // parts that a thread of the last merge asks for at once (12: longer code, 1 to 2 % slower calls)
@@ -414,14 +417,27 @@ template <int DH>
 struct C4Sums {
   float o[PgTile<DH>::NB][2][4];  // [block][16 channels][C fragment]: channels 32 b + 4 g + i (i = 2 x, rows g and g + 8)
   float top0, top1, ref0, ref1, sum0, sum1;
-  int v_exp;         // scales of values are taken 2^v_exp times as large, and so is o: 10 while none is above C4_TINY, 0 up to 2, and what
-  uint32_t v_limit;  // takes them below 2 beyond; fp16 bits of the largest scale that this holds for
+  // Scales of values are taken 2^e times as large, and so is o: e = 10 while none is above C4_TINY, 0 while all are below 2.  Beyond, every block
+  // has an e of its own: that, as long as its scales allow it, and what takes them below 2 then.  v_limit: fp16 bits, in both halves, of the
+  // largest scale that e holds for, from which it follows; where blocks differ, a lane has those of the blocks that it looks at: `lane` modulo
+  // the blocks, at 256 channels twice that and the next one.
+  uint32_t v_limit[DH == 256 ? 2 : 1];
 };
+__device__ __forceinline__ int c4_exponent(uint32_t limit) { return 16 - static_cast<int>(((limit & 0xffffu) + 1) >> 10); }
+// what the lane that has block b says of it
+template <int DH, class X>
+__device__ __forceinline__ X c4_of_block(const X (&own)[DH == 256 ? 2 : 1], int b) {
+  if constexpr (DH == 256) return __shfl_sync(0xffffffffu, own[b & 1], b >> 1);
+  else return __shfl_sync(0xffffffffu, own[0], b);
+}
+// two scales, those that are no numbers left out
+__device__ __forceinline__ uint32_t c4_numbers(uint32_t w) { return ((w & 0xffffu) <= 0x7c00u ? w & 0xffffu : 0u) | (w >> 16 <= 0x7c00u ? w & 0xffff0000u : 0u); }
 
-// NT tiles at once.  EDGE: tokens that are not seen are left out (the first one at `pos`); otherwise all are seen.
-template <int DH, int NT, bool EDGE, int QB>
-__device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *query, const uint32_t (&qf)[QB][4], float qs0, float qs1, const C4Span &sp,
-                                          int pos, bool first, int lane, C4Sums<DH> &A) {
+// NT tiles at once.  EDGE: tokens that are not seen are left out (the first one at `pos`); otherwise, and without `edge`, all are seen.  Without
+// LARGE: false, and nothing done, where a scale of 2 or more is seen.  With it, scales times 2^e take their place in the tile.
+template <int DH, int NT, bool EDGE, bool LARGE, int QB>
+__device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, const uint32_t (&qf)[QB][4], float qs0, float qs1, const C4Span &sp,
+                                          int pos, bool first, int lane, C4Sums<DH> &A, bool edge = true) {
   typedef PgTile<DH> T;
   constexpr int NB = T::NB, BH = T::BH;
   const int g = lane >> 2, t = lane & 3;
@@ -467,33 +483,33 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
     s[x][1] *= qs1;
     s[x][2] *= qs0;
     s[x][3] *= qs1;
-    if (EDGE) {
+    if (EDGE && edge) {
       const int at = pos + x * PG_TILE;
       if (!seen(at + g)) s[x][0] = s[x][1] = -INFINITY;
       if (!seen(at + g + 8)) s[x][2] = s[x][3] = -INFINITY;
     }
   }
-  // ---- the largest scale of the values, as whole numbers (none is negative): every lane looks at some
-  uint32_t over = 0;  // whether one is above the limit; at an edge: the largest that is seen and finite
-  if (EDGE) {
-    const int token = (lane >> 2) * 2 + (lane >> 1 & 1);
+  // ---- whether a scale of the values is above its limit, as whole numbers (none is negative): a lane looks at two tokens of a block, or of two; at
+  // an edge at those that are seen
+  constexpr int VB = DH == 256 ? 2 : 1, LANES = DH == 64 ? 2 : 4;  // blocks of a lane; lanes that have different ones
+  const int word0 = DH == 64 ? lane & 15 : VB * lane;
+  uint32_t own[NT][VB], over = 0;
 #pragma unroll
-    for (int x = 0; x < NT; ++x)
-#pragma unroll
-      for (int j = 0; j < NB / 2; ++j) {
-        const uint32_t h = *reinterpret_cast<const uint16_t *>(tile0 + x * T::BYTES + T::VS + ((lane >> 2) * NB + j * 2 + (lane & 1)) * 4 + (lane >> 1 & 1) * 2);
-        if (h <= 0x7c00 && seen(pos + x * PG_TILE + token)) over = max(over, h);
-      }
-  } else {
+  for (int x = 0; x < NT; ++x) lds_words<VB>(tile0 + x * T::BYTES + T::VS + word0 * 4, own[x]);
+  if (EDGE && edge) {
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
-      if (DH == 256) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(tile0 + x * T::BYTES + T::VS + lane * 8);
-        over = __vimax3_u16x2(over, w.x, w.y);
-      } else {
-        over = __vimax3_u16x2(over, 0u, *reinterpret_cast<const uint32_t *>(tile0 + x * T::BYTES + T::VS + (DH == 128 ? lane : lane & 15) * 4));
-      }
+      const int token = pos + x * PG_TILE + word0 / NB * 2;
+#pragma unroll
+      for (int j = 0; j < VB; ++j) own[x][j] &= (seen(token) ? 0xffffu : 0u) | (seen(token + 1) ? 0xffff0000u : 0u);
     }
+  }
+#pragma unroll
+  for (int j = 0; j < VB; ++j) {
+    uint32_t most = A.v_limit[j];
+#pragma unroll
+    for (int x = 0; x < NT; ++x) most = __vmaxu2(most, own[x][j]);
+    over |= most ^ A.v_limit[j];
   }
   // ---- the reference moves when a score exceeds it by 3, so that weights stay within 2^15; scales stay below 2
   float tm0 = fmaxf(s[0][0], s[0][2]), tm1 = fmaxf(s[0][1], s[0][3]);
@@ -502,30 +518,43 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
     tm0 = fmax3(tm0, s[x][0], s[x][2]);
     tm1 = fmax3(tm1, s[x][1], s[x][3]);
   }
-  if (__any_sync(0xffffffffu, tm0 - A.top0 > 3.0f || tm1 - A.top1 > 3.0f || (over & 0xffffu) > A.v_limit || (over >> 16) > A.v_limit)) {
+  if (__any_sync(0xffffffffu, tm0 > __fadd_rd(A.top0, 3.0f) || tm1 > __fadd_rd(A.top1, 3.0f) || over != 0)) {
     float n0 = tm0, n1 = tm1;
 #pragma unroll
     for (int d = 4; d < 32; d *= 2) {
       n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, d));
       n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, d));
     }
-    if (!EDGE) {  // (a NaN moves nothing, and hides nothing)
-      over = 0;
+    // (a NaN among the scales moves nothing, and hides nothing)
+    auto largest = [&](int j, auto some) {
+      uint32_t most = 0;
 #pragma unroll
-      for (int x = 0; x < NT; ++x)
+      for (int x = 0; x < NT; ++x) most = __vmaxu2(most, some(own[x][j]));
+      return max(most & 0xffffu, most >> 16);
+    };
+    int shift[VB] = {};  // of the exponents
+    if (LARGE) {
 #pragma unroll
-        for (int j = 0; j < NB / 2; ++j) {
-          const uint32_t h = *reinterpret_cast<const uint16_t *>(tile0 + x * T::BYTES + T::VS + (j * 32 + lane) * 2);
-          if (h <= 0x7c00) over = max(over, h);
-        }
-    }
-    over = __reduce_max_sync(0xffffffffu, over);
-    float back = 1.0f;
-    if (over > A.v_limit) {
-      const int e = max(static_cast<int>(over >> 10) - 14, 1);  // scales below 2^e
-      A.v_limit = ((e + 15) << 10) - 1;
-      back = __int_as_float((127 + 1 - e - A.v_exp) << 23);
-      A.v_exp = 1 - e;
+      for (int j = 0; j < VB; ++j) {
+        uint32_t most = largest(j, c4_numbers);
+#pragma unroll
+        for (int d = LANES; d < 32; d *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+        const int e = c4_exponent(A.v_limit[j]);
+        if (most > (A.v_limit[j] & 0xffffu)) A.v_limit[j] = ((max(static_cast<int>(most >> 10) - 14, 1) + 15) * 1024 - 1) * 0x10001u;  // (scales below 2^1, 2^2, ...)
+        shift[j] = c4_exponent(A.v_limit[j]) - e;
+      }
+    } else {
+      auto all = [&](auto some) { return __reduce_max_sync(0xffffffffu, VB == 2 ? max(largest(0, some), largest(VB - 1, some)) : largest(0, some)); };
+      uint32_t most = all([](uint32_t w) { return w; });
+      if (most > C4_USUAL) {
+        most = all(c4_numbers);
+        if (most > C4_USUAL) return false;
+      }
+      if (most > C4_TINY && A.v_limit[0] == C4_TINY * 0x10001u) {
+#pragma unroll
+        for (uint32_t &limit : A.v_limit) limit = C4_USUAL * 0x10001u;
+        shift[0] = -10;
+      }
     }
     n0 = fmaxf(n0, A.top0);
     n1 = fmaxf(n1, A.top1);
@@ -538,9 +567,9 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
     if (!first) {
       A.sum0 *= c0;
       A.sum1 *= c1;
-      const float o0 = c0 * back, o1 = c1 * back;
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b) {
+        const float back = __int_as_float((127 + (LARGE ? c4_of_block<DH>(shift, b) : shift[0])) << 23), o0 = c0 * back, o1 = c1 * back;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           A.o[b][x][0] *= o0;
@@ -548,6 +577,7 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
           A.o[b][x][2] *= o0;
           A.o[b][x][3] *= o1;
         }
+      }
     }
   }
   // ---- weights, and the values times them
@@ -560,43 +590,79 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
     w[x][0] = as_half2(transpose8(as_word(__floats2half2_rn(p0, p1))));
     w[x][1] = as_half2(transpose8(as_word(__floats2half2_rn(p2, p3))));
   }
-  const bool scaled = A.v_exp != 0;
-  const __half2 up = __float2half2_rn(__int_as_float((127 + A.v_exp) << 23));
+  const bool tiny = !LARGE && A.v_limit[0] != C4_USUAL * 0x10001u;
+  auto add_values = [&]() {
 #pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    const uint8_t *tile = tile0 + x * T::BYTES;
-    uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
-    if (EDGE) {
-      const int at = pos + x * PG_TILE;
-      keep0 = (seen(at + 2 * t) ? 0xffffu : 0u) | (seen(at + 2 * t + 1) ? 0xffff0000u : 0u);
-      keep1 = (seen(at + 2 * t + 8) ? 0xffffu : 0u) | (seen(at + 2 * t + 9) ? 0xffff0000u : 0u);
-    }
+    for (int x = 0; x < NT; ++x) {
+      const uint8_t *tile = tile0 + x * T::BYTES;
+      uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
+      if (EDGE && edge) {
+        const int at = pos + x * PG_TILE;
+        keep0 = (seen(at + 2 * t) ? 0xffffu : 0u) | (seen(at + 2 * t + 1) ? 0xffff0000u : 0u);
+        keep1 = (seen(at + 2 * t + 8) ? 0xffffu : 0u) | (seen(at + 2 * t + 9) ? 0xffff0000u : 0u);
+      }
 #pragma unroll
-    for (int hf = 0; hf < T::HALVES; ++hf) {
-      uint32_t vw[2][BH], vs[2][BH];  // scales: fp16 of tokens 2 t, 2 t + 1 and of 2 t + 8, 2 t + 9
-      lds_words<BH>(tile + T::VS + t * (NB * 4) + hf * (BH * 4), vs[0]);
-      lds_words<BH>(tile + T::VS + (t + 4) * (NB * 4) + hf * (BH * 4), vs[1]);
-      lds_words<BH>(tile + T::V + hf * (64 * T::W) + lane * T::W, vw[0]);
-      lds_words<BH>(tile + T::V + hf * (64 * T::W) + 32 * T::W + lane * T::W, vw[1]);
-      if (scaled) {
+      for (int hf = 0; hf < T::HALVES; ++hf) {
+        uint32_t vw[2][BH], vs[2][BH];  // scales: fp16 of tokens 2 t, 2 t + 1 and of 2 t + 8, 2 t + 9
+        lds_words<BH>(tile + T::VS + t * (NB * 4) + hf * (BH * 4), vs[0]);
+        lds_words<BH>(tile + T::VS + (t + 4) * (NB * 4) + hf * (BH * 4), vs[1]);
+        lds_words<BH>(tile + T::V + hf * (64 * T::W) + lane * T::W, vw[0]);
+        lds_words<BH>(tile + T::V + hf * (64 * T::W) + 32 * T::W + lane * T::W, vw[1]);
+        if (tiny) {
+#pragma unroll
+          for (int bb = 0; bb < BH; ++bb) {
+            vs[0][bb] = as_word(__hmul2(as_half2(vs[0][bb]), __float2half2_rn(0x1p10f)));
+            vs[1][bb] = as_word(__hmul2(as_half2(vs[1][bb]), __float2half2_rn(0x1p10f)));
+          }
+        }
 #pragma unroll
         for (int bb = 0; bb < BH; ++bb) {
-          vs[0][bb] = as_word(__hmul2(as_half2(vs[0][bb]), up));
-          vs[1][bb] = as_word(__hmul2(as_half2(vs[1][bb]), up));
+          const int b = hf * BH + bb;
+          uint32_t lo[4], hi[4];
+          e2m1_word(vw[0][bb], lo);
+          e2m1_word(vw[1][bb], hi);
+          const uint32_t b0 = as_word(__hmul2(w[x][0], as_half2(vs[0][bb] & keep0))), b1 = as_word(__hmul2(w[x][1], as_half2(vs[1][bb] & keep1)));
+          mma_f16(A.o[b][0], lo[0], lo[1], hi[0], hi[1], b0, b1);
+          mma_f16(A.o[b][1], lo[2], lo[3], hi[2], hi[3], b0, b1);
         }
       }
+    }
+  };
+  if (!LARGE) {
+    add_values();
+    return true;
+  }
+  // Scales that have no room in fp16 times 2^e (with e < 0, below 2^-19: they have six bits) are left to a second turn, 2^16 times as
+  // large and with weights 2^16 times as small, of which they lose 2^-28 at most.  A lane has its words to itself.
+  bool small = false;
+  auto rescale = [&](bool second) {
+    __syncwarp();  // (every lane has read the tile)
 #pragma unroll
-      for (int bb = 0; bb < BH; ++bb) {
-        const int b = hf * BH + bb;
-        uint32_t lo[4], hi[4];
-        e2m1_word(vw[0][bb], lo);
-        e2m1_word(vw[1][bb], hi);
-        const uint32_t b0 = as_word(__hmul2(w[x][0], as_half2(vs[0][bb] & keep0))), b1 = as_word(__hmul2(w[x][1], as_half2(vs[1][bb] & keep1)));
-        mma_f16(A.o[b][0], lo[0], lo[1], hi[0], hi[1], b0, b1);
-        mma_f16(A.o[b][1], lo[2], lo[3], hi[2], hi[3], b0, b1);
+    for (int j = 0; j < VB; ++j) {
+      const int e = c4_exponent(A.v_limit[j]);
+      const uint32_t room = e >= 0 ? 0u : e > -6 ? 1u << (5 - e) : static_cast<uint32_t>(-4 - e) << 10;  // fp16 bits of 2^(-19 - e)
+      const __half2 up = __float2half2_rn(__int_as_float((127 + (second ? min(e + 16, 15) : e)) << 23));
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        const uint32_t low = ((own[x][j] & 0xffffu) < room ? 0xffffu : 0u) | (own[x][j] >> 16 < room ? 0xffff0000u : 0u);
+        small = small || (own[x][j] & low) != 0;
+        *reinterpret_cast<uint32_t *>(tile0 + x * T::BYTES + T::VS + (word0 + j) * 4) = as_word(__hmul2(as_half2(own[x][j] & (second ? low : ~low)), up));
       }
     }
+    fence_proxy_async_smem();  // (the next copy into the stage comes behind this)
+    __syncwarp();
+  };
+  rescale(false);
+  add_values();
+  if (__any_sync(0xffffffffu, small)) {
+    rescale(true);
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) w[x][h] = __hmul2(w[x][h], __float2half2_rn(0x1p-16f));
+    add_values();
   }
+  return true;
 }
 
 // The tiles of a sequence and KV head are cut into equal runs, one a CTA, of at least a tile for each warp and not more of them than the
@@ -610,9 +676,11 @@ __device__ __forceinline__ void c4_attend(const uint8_t *tile0, const uint8_t *q
 //
 // Codes become fp16 exactly and are multiplied as they are: keys (16 x 16 channels a step) with the queries, and the scores of every
 // block of 32 channels with its scale in fp32; values, transposed by the way they are stored, with the softmax weights times
-// their token's scale.  The weights are 2^(s - m'), m' = the reference maximum less 12 (c4_reference), and scales that are all below 2^-9, or some of
-// them 2 or more, are taken a power of two times as large, so that fp16 rounds a weight and its product like any other down to
-// 2^-26 of the largest one.
+// their token's scale.  The weights are 2^(s - m'), m' = the reference maximum less 12 (c4_reference): fp16 rounds a weight like any other
+// down to 2^-26 of the largest one.  So that it does the same to the products with scales, these are taken 2^10 times as large where none of the head
+// is 2^-9 or more, and from the first one of 2 on each block's by a power of two that takes the largest below 2, in a loop of its own
+// (values of deviation 30: 32.6 us for 16 x 8192 keys of a Qwen3-4B layer, 30.9 otherwise; 18.1 and 15.2 for 32768 of a Gemma-3-4B one; with one power for the
+// whole head, which loses the small ones, 30.8 and 15.4).  One that this leaves below 2^-19 is left to a second turn over the tile.
 //
 // 16 x 8192 keys, 32 query on 8 KV heads of 128: 31.4 us for 146 MB (16-bit caches of the same keys take 106).  44 of 57 thousand clocks
 // are the tiles, at 6.3 TB/s: bound by memory then, at 2 to 3 instructions a clock and SM (2 products, 8 conversions and some 6
@@ -839,38 +907,62 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
         for (int i = 0; i < 4; ++i) A.o[b][x][i] = 0.f;
     A.top0 = A.top1 = -INFINITY;
     A.ref0 = A.ref1 = A.sum0 = A.sum1 = 0.f;
-    A.v_exp = 10;
-    A.v_limit = C4_TINY;
+#pragma unroll
+    for (uint32_t &limit : A.v_limit) limit = C4_TINY * 0x10001u;
     const int plain0 = s_span[seq].plain0, plain1 = s_span[seq].plain1;
-    bool first = true;
+    // The parts of the run, up to one with a scale of 2 or more; with `Large` the tiles from there on.
+    bool first = true, large = false;
+    int ahead = 0;  // tiles of the part that have been attended
+    auto parts = [&](auto Large) {
+      constexpr bool LARGE = decltype(Large)::value, PLAIN = !LARGE || DH == 128;
 #pragma unroll 1
-    while (i < end) {
-      const uint32_t stage = attended % S;
-      if (!__all_sync(0xffffffffu, mbar_try_wait(bars + 8 * stage, (attended / S) & 1)) &&
-          !warp_wait(bars + 8 * stage, (attended / S) & 1, &s_abort, P.timeout_ns, lane)) {
-        raise(P.status, STATUS_TIMEOUT, &s_abort);
-        // the copies in flight still land in this CTA's memory; the warp goes on through the merges, whose barriers count it
-        timed_out = true;
-        for (int j = i / TP * TP; j < min(end, i / TP * TP + S * TP); j += TP, ++attended)
-          warp_wait(bars + 8 * (attended % S), (attended / S) & 1, &s_abort, P.timeout_ns, lane);
-        break;
-      }
-      const int next = min(end, i / TP * TP + TP);
-      const uint8_t *at = ring + stage * C::STAGE;
-      if (!(unusable >> stage & 1)) {
-        if (next - i == TP && i >= plain0 && next <= plain1) {
-          c4_attend<DH, TP, false>(at, query, qf, qs0, qs1, s_span[seq], 0, first, lane, A);
-        } else {
-#pragma unroll 1
-          for (int x = i; x < next; ++x) c4_attend<DH, 1, true>(at + (x - i) * T::BYTES, query, qf, qs0, qs1, s_span[seq], s_span[seq].pos(x), first && x == i, lane, A);
+      while (i < end) {
+        const uint32_t stage = attended % S;
+        if (!__all_sync(0xffffffffu, mbar_try_wait(bars + 8 * stage, (attended / S) & 1)) &&
+            !warp_wait(bars + 8 * stage, (attended / S) & 1, &s_abort, P.timeout_ns, lane)) {
+          raise(P.status, STATUS_TIMEOUT, &s_abort);
+          // the copies in flight still land in this CTA's memory; the warp goes on through the merges, whose barriers count it
+          timed_out = true;
+          for (int j = i / TP * TP; j < min(end, i / TP * TP + S * TP); j += TP, ++attended)
+            warp_wait(bars + 8 * (attended % S), (attended / S) & 1, &s_abort, P.timeout_ns, lane);
+          return;
         }
-        first = false;
+        const int next = min(end, i / TP * TP + TP);
+        uint8_t *at = ring + stage * C::STAGE;
+        if (LARGE) {
+          at += ahead * T::BYTES;
+          ahead = 0;
+        }
+        if (!(unusable >> stage & 1)) {
+          if (PLAIN && next - i == TP && i >= plain0 && next <= plain1) {
+            if (!c4_attend<DH, TP, false, LARGE>(at, query, qf, qs0, qs1, s_span[seq], 0, first, lane, A)) {
+              large = true;
+              return;
+            }
+          } else {
+#pragma unroll 1
+            for (int x = i; x < next; ++x) {
+              // (one tile at a time for both kinds, but for 128 channels: two plain ones at once 32.6 us, one 40.6)
+              if (!c4_attend<DH, 1, true, LARGE>(at + (x - i) * T::BYTES, query, qf, qs0, qs1, s_span[seq], s_span[seq].pos(x), first && x == i, lane, A,
+                                                  !LARGE || x < plain0 || x >= plain1)) {
+                large = true;
+                ahead = x - i;
+                i = x;
+                first = first && ahead == 0;
+                return;
+              }
+            }
+          }
+          first = false;
+        }
+        i = next;
+        __syncwarp();
+        fetch(i / TP * TP + (S - 1) * TP, stage);
+        ++attended;
       }
-      i = next;
-      __syncwarp();
-      fetch(i / TP * TP + (S - 1) * TP, stage);
-      ++attended;
-    }
+    };
+    parts(std::false_type());
+    if (large) parts(std::true_type());
     // ---- the next run is asked for before the warps' sums of this one come together
     const bool whole = run1 - run0 == s_span[seq].tiles;
     const long long out0 = static_cast<long long>(seq) * P.n_q + head * P.group;  // rows of the output
@@ -893,14 +985,15 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
       s_ml[warp][2 * t] = make_float2(A.top0 == -INFINITY ? -INFINITY : A.ref0, A.sum0);
       s_ml[warp][2 * t + 1] = make_float2(A.top1 == -INFINITY ? -INFINITY : A.ref1, A.sum1);
     }
-    if (A.v_exp != 0) {
-      const float down = __int_as_float((127 - A.v_exp) << 23);
+    if (large || A.v_limit[0] != C4_USUAL * 0x10001u) {
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b) {
+        const float down = __int_as_float((127 - c4_exponent(c4_of_block<DH>(A.v_limit, b))) << 23);
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int e = 0; e < 4; ++e) A.o[b][x][e] *= down;
+      }
     }
 #pragma unroll 1
     for (int h0 = 0; h0 < P.group; h0 += C::HEADS) {

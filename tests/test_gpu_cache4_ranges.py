@@ -4,8 +4,8 @@ some blocks or tokens are many powers of two larger than others.  The bound is t
 Tolerances.  A weight is rounded to fp16 (2^-11 of itself), its product with the scale of its token and block again (2^-11), the output once.  Weights are
 2^12 times as large as those of the definition over the largest of them, or more, before the division by their sum (which is 2^12 at least).  One that is
 below 2^-14 all the same, 2^-26 of the largest, is off by 2^-25 instead: by 2^-37, times its value |v|.  The product is taken with the scale over U,
-U = 2^-10 while none of the block's scales is 2^-9 or more, 1 while all are below 2, else a power of two between half the largest scale
-S and S.  Where it is below 2^-14 (weight over the largest, times scale over U, below 2^-26) it is off by 2^-25, which is 2^-37 U in the output, times a step of at most 6.
+U = 2^-10 while none of the head's scales is 2^-9 or more, 1 while all of the block's are below 2, else a power of two between half the block's
+largest scale S and S.  Where it is below 2^-14 (weight over the largest, times scale over U, below 2^-26) it is off by 2^-25, which is 2^-37 U in the output, times a step of at most 6.
 So a block's error is at most
     (2^-10 + 2^-14) sum_j p_j |v_j| + half a step of the output + 2^-37 (sum of |v_j| over such weights + 6 U times the number of such products)
 with 2^-14 for the scores' fp32 sums (256 products of magnitude 8 at most, in blocks of 32, 2^-24 of the running sum each, times ln 2).  Where scores are 2^18 or more
@@ -32,7 +32,7 @@ def per_block(got, q, k, v, scale, lost=False):
     rel = (p / p.amax(-1, keepdim=True)).T[:, :, None]                                                  # [tokens, heads, 1]
     top = v.abs().unflatten(-1, (-1, 32)).amax(-1).repeat_interleave(group, 1)                          # [tokens, heads, blocks]: 4 to 6 times the scale
     most = top.amax(0) / 4
-    U = torch.maximum(torch.where(most < 2**-9, 2**-10, 1.0), most)
+    U = torch.maximum(torch.where(most.amax(-1, keepdim=True) < 2**-9, 2**-10, 1.0), most)
     low = ((rel < 2.0**(-14 - bits)) * top).sum(0) + 6 * U * ((rel * (top / 6) / U < 2.0**(-14 - bits)) & (top > 0)).sum(0)
     bound = (2**-10 + 2**-14) * mass + torch.finfo(got.dtype).eps / 2 * out.abs() + torch.finfo(got.dtype).smallest_normal * torch.finfo(got.dtype).eps
     bound = bound + (2.0**(-25 - bits) * low).repeat_interleave(32, 1)
@@ -81,3 +81,47 @@ def test_scores_whose_neighbours_are_far_apart(shape, dtype, power, order):
             k, q = k.to(DT[dtype]), q.to(DT[dtype])
             assert torch.equal(held(k), k.double())
             run(shape, dtype, k, rows(power, n, nkv, dh, dtype), q, LN2, power >= 18)
+
+
+# ------------------------------------------------------------------------------------------------ values
+@pytest.mark.parametrize("shape,dtype", [("g1", 0), ("g1", 1), ("gemma", 0), ("gemma", 1), ("g8-64", 0), ("g8-64", 1), ("qwen", 0)])
+@pytest.mark.parametrize("large", [6e4, 3e4, 1000.0, 20.0])
+@pytest.mark.parametrize("where", ["start", "end", "all"])
+def test_a_block_of_large_values_beside_small_ones(shape, dtype, large, where):
+    """One block of a head holds large values, in the first tokens, the last ones or all; the others of the head 1e-3, 1e-2, ... : each is
+    as exact as without it."""
+    nq, nkv, dh = SHAPES[shape]
+    for n in (600, 21):
+        v = rows(5, n, nkv, dh, dtype).float().clamp(-3, 3) / 3
+        v *= torch.tensor([1e-3, 1e-2, 1e-4, 0.3], device="cuda")[torch.arange(dh, device="cuda") // 32 % 4]
+        some = {"start": slice(0, 5), "end": slice(n - 5, n), "all": slice(0, n)}[where]
+        block = 1 if dh == 64 else 3
+        v[some, :, 32 * block:32 * block + 32] = (rows(6, n, nkv, 32, dtype).float().clamp(-3, 3) / 3 * large)[some]
+        run(shape, dtype, rows(7, n, nkv, dh, dtype), v.to(DT[dtype]), rows(8, 1, nq, dh, dtype), 0.0)
+
+
+@pytest.mark.parametrize("shape,dtype", [("g1", 0), ("gemma", 1), ("g8-64", 0), ("qwen", 1)])
+@pytest.mark.parametrize("at", [0, 333, 599])
+def test_a_token_of_large_values_that_weighs_nothing(shape, dtype, at):
+    """A token whose values are 2^25 times as large as the others', in all blocks, and whose weight is 0: the others come out as exact as without it."""
+    nq, nkv, dh = SHAPES[shape]
+    n = 600
+    q = rows(11, 1, nq, dh, dtype)
+    k = rows(12, n, nkv, dh, dtype, 0.3).float()
+    k[at] = -8 * q[0].view(nkv, nq // nkv, dh)[:, 0].float()
+    q = q.view(nkv, nq // nkv, dh)[:, :1].expand(nkv, nq // nkv, dh).reshape(1, nq, dh).contiguous()
+    v = rows(13, n, nkv, dh, dtype, 1e-3).float()
+    v[at] = 3e4
+    run(shape, dtype, k.to(DT[dtype]), v.to(DT[dtype]), q, 0.0)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_blocks_of_every_size(dtype):
+    """The blocks of a head are 2^4 apart, from the smallest scales to the largest, and each one's values change by 2^6 along the sequence."""
+    nq, nkv, dh = SHAPES["gemma"]
+    n = 900
+    size = torch.exp2(4.0 * (torch.arange(dh, device="cuda") // 32) - (16 if dtype else 20))
+    ramp = torch.exp2(6 * torch.linspace(-0.5, 0.5, n, device="cuda"))[:, None, None]
+    v = rows(21, n, nkv, dh, 0).float() * size
+    for along in (ramp, ramp.flip(0)):
+        run("gemma", dtype, rows(22, n, nkv, dh, dtype), (v * along).clamp(-6e4, 6e4).to(DT[dtype]), rows(23, 1, nq, dh, dtype), 0.0)
