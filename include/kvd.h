@@ -649,8 +649,8 @@ kvd_status kvd_decode_attention_static(int n_q_heads, int n_kv_heads, int d_head
 /* Fill `out` with the byte counts described at kvd_mem_stats. */
 kvd_status kvd_memory_stats(const kvd_ctx *ctx, kvd_mem_stats *out);
 
-/* Wait for `stream`, read and clear the device status word.  KVD_OK, KVD_ERR_TIMEOUT, KVD_ERR_POSITION, KVD_ERR_CAPACITY (pages that
- * ran out) or (checking build) KVD_ERR_BOUNDS. */
+/* Wait for `stream`, read and clear the device status word.  KVD_OK, or the first of KVD_ERR_TIMEOUT, (checking build) KVD_ERR_BOUNDS,
+ * KVD_ERR_CAPACITY (pages that ran out; what the rest of such a step records of its positions of -1 goes with it) and KVD_ERR_POSITION. */
 kvd_status kvd_poll_status(kvd_ctx *ctx, void *stream);
 
 /* Self-test of the failure path: enqueue a one-thread kernel that waits (at most limit_ms, 1..1000)

@@ -1418,8 +1418,8 @@ extern "C" kvd_status kvd_poll_status(kvd_ctx *ctx, void *stream_) {
   }
   if (word & STATUS_TIMEOUT) return KVD_ERR_TIMEOUT;
   if (word & STATUS_BOUNDS) return KVD_ERR_BOUNDS;
+  if (word & STATUS_CAPACITY) return KVD_ERR_CAPACITY;  // (a step without room goes on with positions of -1)
   if (word & STATUS_POSITION) return KVD_ERR_POSITION;
-  if (word & STATUS_CAPACITY) return KVD_ERR_CAPACITY;
   return KVD_OK;
 }
 
