@@ -706,7 +706,7 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
   __shared__ float2 s_ml[WARPS][8];         // maximum and sum of a warp and head
   __shared__ int2 s_parted[2];
   __shared__ int s_last[2];
-  __shared__ volatile int s_abort;
+  __shared__ volatile int s_abort, s_never;  // (a flag that nobody raises)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, t = lane & 3;
   uint8_t *ring = smem + warp * (S * C::STAGE), *query = smem + C::RING;
@@ -716,7 +716,7 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
     for (int i = 0; i < S; ++i) mbar_init(bars + 8 * i, 1);
     fence_mbar_init();
   }
-  if (tid == 0) s_abort = 0;
+  if (tid == 0) s_abort = s_never = 0;
   grid_launch_dependents();
   grid_dependency_wait();
   const int pairs = P.n * P.n_kv, grid = gridDim.x, spare = grid - pairs;
@@ -921,10 +921,11 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
         if (!__all_sync(0xffffffffu, mbar_try_wait(bars + 8 * stage, (attended / S) & 1)) &&
             !warp_wait(bars + 8 * stage, (attended / S) & 1, &s_abort, P.timeout_ns, lane)) {
           raise(P.status, STATUS_TIMEOUT, &s_abort);
-          // the copies in flight still land in this CTA's memory; the warp goes on through the merges, whose barriers count it
+          // The copies in flight land before the CTA's shared memory goes to another: each is waited for once more, whatever the abort flag
+          // says.  The warp goes on through the merges, whose barriers count it.
           timed_out = true;
           for (int j = i / TP * TP; j < min(end, i / TP * TP + S * TP); j += TP, ++attended)
-            warp_wait(bars + 8 * (attended % S), (attended / S) & 1, &s_abort, P.timeout_ns, lane);
+            warp_wait(bars + 8 * (attended % S), (attended / S) & 1, &s_never, P.timeout_ns, lane);
           return;
         }
         const int next = min(end, i / TP * TP + TP);
