@@ -74,6 +74,8 @@ __device__ __forceinline__ T *peer(T *p, unsigned rank) {
   return reinterpret_cast<T *>(a);
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+// Until the other CTAs' threads have ended or come here too (of threads that have ended nothing is awaited); threads of a warp need not be together.
+__device__ __forceinline__ void cluster_stay() { asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory"); }
 // Until a barrier's messages have come; false: the time is up, or another thread's was.  Other CTAs complete it, so the wait acquires at
 // cluster scope.
 static __device__ __noinline__ bool await_slow(uint32_t bar, const volatile int *abort_flag, unsigned long long timeout_ns) {
@@ -299,6 +301,10 @@ __global__ void __launch_bounds__(SM_THREADS, 1) kvd_sample_kernel(const __grid_
   const float asked_p = P.top_p ? P.top_p[r] : 1.0f, asked_m = P.min_p ? P.min_p[r] : 0.0f, u = P.u[r];
   const bool greedy = !(temp > 0.0f);
   const int share0 = min(P.n, static_cast<int>(rank) * P.share), share1 = min(P.n, share0 + P.share);
+  // A CTA with a thread that has given up a wait keeps its memory until the others have ended: they still read it and send messages there.
+  auto leave = [&]() {
+    if (s_abort != 0) cluster_stay();
+  };
   auto heard = [&](int what) {  // (a message that does not come: recorded, and the row has no token)
     if (await(smem_u32(&S.arrived[what]), &s_abort, P.timeout_ns)) return;
     raise(P.status, STATUS_TIMEOUT, &s_abort);
@@ -816,10 +822,16 @@ __global__ void __launch_bounds__(SM_THREADS, 1) kvd_sample_kernel(const __grid_
   int owner = -1;
 #pragma unroll
   for (int p = CTAS - 1; p >= 0; --p) owner = reach[p] > target ? p : owner;
-  if (owner != static_cast<int>(rank)) return;
+  if (owner != static_cast<int>(rank)) {
+    leave();
+    return;
+  }
   const uint64_t run_in = share_from + above_in + min(ties_in, share_left) * mass_t;  // up to the end of run `lane`
   const int own = __ffs(__ballot_sync(NONE, run_in > target)) - 1;
-  if (own < 0) return;  // (a message did not come)
+  if (own < 0) {  // (a message did not come)
+    leave();
+    return;
+  }
   uint64_t m = own > 0 ? __shfl_sync(NONE, run_in, own - 1) : share_from;
   unsigned quota = share_left;
   const unsigned ties_before = own > 0 ? __shfl_sync(NONE, ties_in, own - 1) : 0u;
@@ -873,6 +885,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) kvd_sample_kernel(const __grid_
     m += all + n * mass_t;
     quota -= n;
   }
+  leave();
 }
 
 }  // namespace kvd

@@ -16,3 +16,14 @@ def test_copies_of_the_cache_are_waited_for_whatever_the_abort_flag_says():
     assert re.findall(r"s_never\s*=[^;]*;", body) == ["s_never = 0;"] and body.count("s_never") == 2 + len(waits)
     # all parts that may be on their way: as many as the ring has stages
     assert re.search(r"for \(int j = i / TP \* TP; j < min\(end, i / TP \* TP \+ S \* TP\); j \+= TP, \+\+attended\)", given_up)
+
+
+def test_a_cta_of_a_cluster_keeps_its_memory_for_the_others():
+    body = KERNELS["kvd_sample_kernel"][1]
+    assert re.search(r"auto leave = \[&\]\(\) \{\s*if \(s_abort != 0\) cluster_stay\(\);\s*\};", body)
+    # behind the last wait every way out goes by it (the way out before is that of a row without a message, behind a barrier of all)
+    behind = body[body.index("heard(SM_SHARES);"):]
+    ways = len(re.findall(r"\breturn;", behind)) + 1
+    assert len(re.findall(r"leave\(\);\s*(?:return;|\}\s*$)", behind)) == ways == 3
+    before = body[:body.index("heard(SM_SUMS);")]
+    assert re.search(r"cluster_wait\(\);\s*return;", before)
