@@ -892,26 +892,57 @@ __global__ void __launch_bounds__(SM_THREADS, 1) kvd_sample_kernel(const __grid_
 
 using namespace kvd;
 
+// A launch of m rows.  cudaFuncSetAttribute goes before it, and before the question how many clusters the device holds.
+template <int F16, int CTAS>
+struct SampleLaunch {
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr[2];
+  cudaError_t error;
+  SampleLaunch(const kvd_ctx *ctx, int m, cudaStream_t stream) {
+    static std::atomic<bool> configured[64] = {};
+    error = opt_in_smem(ctx, kvd_sample_kernel<F16, CTAS>, SM_SMEM, configured);
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3(m * CTAS, 1, 1);
+    cfg.blockDim = dim3(SM_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = SM_SMEM;
+    cfg.stream = stream;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CTAS;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = (serial_launch_mask() & 8) || 2 * m * CTAS > ctx->num_sms ? 0 : 1;  // (as launch_dependent)
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+  }
+};
+
 template <int F16, int CTAS>
 static cudaError_t launch_sample(kvd_ctx *ctx, const SampleParams &P, int m, cudaStream_t stream) {
-  static std::atomic<bool> configured[64] = {};
-  cudaError_t e = opt_in_smem(ctx, kvd_sample_kernel<F16, CTAS>, SM_SMEM, configured);
-  if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3(m * CTAS, 1, 1);
-  cfg.blockDim = dim3(SM_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = SM_SMEM;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CTAS;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = (serial_launch_mask() & 8) || 2 * m * CTAS > ctx->num_sms ? 0 : 1;  // (as launch_dependent)
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kvd_sample_kernel<F16, CTAS>, P);
+  const SampleLaunch<F16, CTAS> L(ctx, m, stream);
+  return L.error != cudaSuccess ? L.error : cudaLaunchKernelEx(&L.cfg, kvd_sample_kernel<F16, CTAS>, P);
+}
+
+// How many rows the device works on at once with that many CTAs each (asked once per device; 0 where it does not say).  A cluster lies within one of the
+// device's groups of SMs, so these are fewer than SMs over CTAs: of 148 SMs 15 with eight, 33 with four.  One more row waits for a second turn: 16 rows of
+// 49152 logits 41.3 us with eight CTAs each, 20.5 with four; 34 of 151936 53.9 with four, 39.6 with two.
+template <int F16, int CTAS>
+static int rows_at_once(const kvd_ctx *ctx) {
+  static std::atomic<int> known[64] = {};  // one more than the answer
+  std::atomic<int> &mine = known[ctx->device & 63];
+  int n = mine.load(std::memory_order_relaxed);
+  if (n == 0) {
+    const SampleLaunch<F16, CTAS> L(ctx, 1, nullptr);
+    if (L.error != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kvd_sample_kernel<F16, CTAS>, &L.cfg) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+    mine.store(++n, std::memory_order_relaxed);
+  }
+  return n - 1;
+}
+template <int F16>
+static int ctas_of_a_row(const kvd_ctx *ctx, int m) {
+  return m <= rows_at_once<F16, 8>(ctx) ? 8 : m <= rows_at_once<F16, 4>(ctx) ? 4 : 2;
 }
 
 extern "C" kvd_status kvd_scaffold_sample(kvd_ctx *ctx, const void *logits, int64_t row_stride, int m, int n, const float *temperature, const int32_t *top_k,
@@ -923,10 +954,11 @@ extern "C" kvd_status kvd_scaffold_sample(kvd_ctx *ctx, const void *logits, int6
   if (m > 65535 || n > KVD_MAX_SAMPLE_VOCAB) return KVD_ERR_CAPACITY;
   if ((reinterpret_cast<uintptr_t>(logits) & 1u) != 0 || !aligned4({temperature, top_k, top_p, min_p, u, tokens_out, probs_out})) return KVD_ERR_ALIGNMENT;
   const OnDevice here(ctx);
-  // as many CTAs per row as the SMs hold at once (a CTA has its SM to itself), two at least, and no more columns for a CTA than two turns
-  // of counting take
-  int ctas = 2;
-  while (ctas < 8 && (2 * ctas * m <= ctx->num_sms || static_cast<int64_t>(ctas) * 2 * SM_TURN < n)) ctas *= 2;
+  // eight CTAs per row, or four, where the device has room for all rows at once, else two; but no more columns for a CTA than two turns of counting
+  // take
+  const bool f16 = ctx->dtype == KVD_DTYPE_F16;
+  int ctas = f16 ? ctas_of_a_row<1>(ctx, m) : ctas_of_a_row<0>(ctx, m);
+  while (ctas < 8 && static_cast<int64_t>(ctas) * 2 * SM_TURN < n) ctas *= 2;
   SampleParams P;
   P.logits = static_cast<const uint16_t *>(logits);
   P.stride = row_stride;
@@ -942,7 +974,6 @@ extern "C" kvd_status kvd_scaffold_sample(kvd_ctx *ctx, const void *logits, int6
   P.status = ctx->d_status;
   P.timeout_ns = ctx->timeout_ns;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  const bool f16 = ctx->dtype == KVD_DTYPE_F16;
   cudaError_t e;
   if (ctas == 2) e = f16 ? launch_sample<1, 2>(ctx, P, m, stream) : launch_sample<0, 2>(ctx, P, m, stream);
   else if (ctas == 4) e = f16 ? launch_sample<1, 4>(ctx, P, m, stream) : launch_sample<0, 4>(ctx, P, m, stream);
