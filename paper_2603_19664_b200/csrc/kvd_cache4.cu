@@ -608,12 +608,20 @@ __device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, 
         lds_words<BH>(tile + T::VS + (t + 4) * (NB * 4) + hf * (BH * 4), vs[1]);
         lds_words<BH>(tile + T::V + hf * (64 * T::W) + lane * T::W, vw[0]);
         lds_words<BH>(tile + T::V + hf * (64 * T::W) + 32 * T::W + lane * T::W, vw[1]);
-        if (tiny) {
+        // Times the weights: here, or where they are used (16 x 8192 keys of 128 channels 30.5 and 31.3 us, 32768 of 256 channels 15.7 and 15.3).
+        constexpr bool AHEAD = DH < 256;
+        auto weigh = [&](int bb, __half2 up, bool scaled) {
+          __half2 v0 = as_half2(vs[0][bb] & keep0), v1 = as_half2(vs[1][bb] & keep1);
+          if (scaled) v0 = __hmul2(v0, up), v1 = __hmul2(v1, up);
+          vs[0][bb] = as_word(AHEAD ? __hmul2(w[x][0], v0) : v0);
+          vs[1][bb] = as_word(AHEAD ? __hmul2(w[x][1], v1) : v1);
+        };
+        if (!tiny) {
 #pragma unroll
-          for (int bb = 0; bb < BH; ++bb) {
-            vs[0][bb] = as_word(__hmul2(as_half2(vs[0][bb]), __float2half2_rn(0x1p10f)));
-            vs[1][bb] = as_word(__hmul2(as_half2(vs[1][bb]), __float2half2_rn(0x1p10f)));
-          }
+          for (int bb = 0; bb < BH; ++bb) weigh(bb, __half2(), false);
+        } else {
+#pragma unroll
+          for (int bb = 0; bb < BH; ++bb) weigh(bb, __float2half2_rn(0x1p10f), true);
         }
 #pragma unroll
         for (int bb = 0; bb < BH; ++bb) {
@@ -621,7 +629,8 @@ __device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, 
           uint32_t lo[4], hi[4];
           e2m1_word(vw[0][bb], lo);
           e2m1_word(vw[1][bb], hi);
-          const uint32_t b0 = as_word(__hmul2(w[x][0], as_half2(vs[0][bb] & keep0))), b1 = as_word(__hmul2(w[x][1], as_half2(vs[1][bb] & keep1)));
+          const uint32_t b0 = AHEAD ? vs[0][bb] : as_word(__hmul2(w[x][0], as_half2(vs[0][bb])));
+          const uint32_t b1 = AHEAD ? vs[1][bb] : as_word(__hmul2(w[x][1], as_half2(vs[1][bb])));
           mma_f16(A.o[b][0], lo[0], lo[1], hi[0], hi[1], b0, b1);
           mma_f16(A.o[b][1], lo[2], lo[3], hi[2], hi[3], b0, b1);
         }
@@ -679,7 +688,7 @@ __device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, 
 // their token's scale.  The weights are 2^(s - m'), m' = the reference maximum less 12 (c4_reference): fp16 rounds a weight like any other
 // down to 2^-26 of the largest one.  So that it does the same to the products with scales, these are taken 2^10 times as large where none of the head
 // is 2^-9 or more, and from the first one of 2 on each block's by a power of two that takes the largest below 2, in a loop of its own
-// (values of deviation 30: 32.6 us for 16 x 8192 keys of a Qwen3-4B layer, 30.9 otherwise; 18.1 and 15.2 for 32768 of a Gemma-3-4B one; with one power for the
+// (values of deviation 30: 32.8 us for 16 x 8192 keys of a Qwen3-4B layer, 30.5 otherwise; 18.1 and 15.4 for 32768 of a Gemma-3-4B one; with one power for the
 // whole head, which loses the small ones, 30.8 and 15.4).  One that this leaves below 2^-19 is left to a second turn over the tile.
 //
 // 16 x 8192 keys, 32 query on 8 KV heads of 128: 31.4 us for 146 MB (16-bit caches of the same keys take 106).  44 of 57 thousand clocks
@@ -943,7 +952,7 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
           } else {
 #pragma unroll 1
             for (int x = i; x < next; ++x) {
-              // (one tile at a time for both kinds, but for 128 channels: two plain ones at once 32.6 us, one 40.6)
+              // (with LARGE one tile at a time for both kinds, but for 128 channels: two plain ones at once 32.6 us, one 40.6)
               if (!c4_attend<DH, 1, true, LARGE>(at + (x - i) * T::BYTES, query, qf, qs0, qs1, s_span[seq], s_span[seq].pos(x), first && x == i, lane, A,
                                                   !LARGE || x < plain0 || x >= plain1)) {
                 large = true;
