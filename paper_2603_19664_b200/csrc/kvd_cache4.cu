@@ -1,8 +1,6 @@
 // A cache held in 4 bits (kvd.h, kvd_pages.h): writing it, reading it back, and decode attention over it.
 #include <string.h>
 
-#include <type_traits>
-
 #include "kvd_internal.h"
 #include "kvd_pages.h"
 #include "kvd_ptx.cuh"
@@ -608,7 +606,7 @@ __device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, 
         lds_words<BH>(tile + T::VS + (t + 4) * (NB * 4) + hf * (BH * 4), vs[1]);
         lds_words<BH>(tile + T::V + hf * (64 * T::W) + lane * T::W, vw[0]);
         lds_words<BH>(tile + T::V + hf * (64 * T::W) + 32 * T::W + lane * T::W, vw[1]);
-        // Times the weights: here, or where they are used (16 x 8192 keys of 128 channels 30.5 and 31.3 us, 32768 of 256 channels 15.7 and 15.3).
+        // Times the weights: here, or where they are used (16 x 8192 keys of 128 channels 30.3 and 31.3 us, 32768 of 256 channels 15.7 and 15.2).
         constexpr bool AHEAD = DH < 256;
         auto weigh = [&](int bb, __half2 up, bool scaled) {
           __half2 v0 = as_half2(vs[0][bb] & keep0), v1 = as_half2(vs[1][bb] & keep1);
@@ -642,7 +640,8 @@ __device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, 
     return true;
   }
   // Scales that have no room in fp16 times 2^e (with e < 0, below 2^-19: they have six bits) are left to a second turn, 2^16 times as
-  // large and with weights 2^16 times as small, of which they lose 2^-28 at most.  A lane has its words to itself.
+  // large and with weights 2^16 times as small, of which they lose 2^-28 at most.  A lane has its words to itself
+  // (at 64 channels with another one, which writes the same).
   bool small = false;
   auto rescale = [&](bool second) {
     __syncwarp();  // (every lane has read the tile)
@@ -674,6 +673,126 @@ __device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, 
   return true;
 }
 
+// A warp's tiles of a run, i .. end - 1 of the sequence and head, and their copies.  Parts are what it has of TILES aligned tiles; lane l knows the
+// part that begins at or behind tile base + TILES l.
+struct C4Feed {
+  int i, end, base, bytes = 0;
+  const uint8_t *src = nullptr;
+  uint32_t bad = 0, unusable = 0;  // parts without a page, stages that hold one
+  uint32_t attended = 0;           // parts, over all runs
+  bool timed_out = false;
+};
+struct C4Place {
+  int seq, head;   // of the launch
+  uint32_t ring, bars;  // of the warp
+  uint64_t policy;
+};
+template <int DH>
+__device__ __forceinline__ void c4_look_up(const C4Attend &P, const C4Span *spans, const C4Place &W, int lane, C4Feed &F) {
+  typedef PgTile<DH> T;
+  constexpr int TP = C4Cfg<DH>::TILES;
+  const int j = max(F.i, F.base + TP * lane), e = min(F.end, F.base + TP * lane + TP);
+  bool bad = false;
+  F.bytes = 0;
+  if (j < e) {
+    const int pos = spans[W.seq].pos(j);
+    const int page = P.table[static_cast<long long>(P.seq[W.seq]) * P.max_pages + pos / PG_TOKENS];
+    bad = page < 0 || page >= P.pages;
+    F.bytes = bad ? 0 : (e - j) * T::BYTES;
+    F.src = P.pool + (bad ? 0 : page) * P.page_bytes + (W.head * PG_TILES + j % PG_TILES) * T::BYTES;
+    if (bad) atomicOr(P.status, STATUS_POSITION);
+    if (!KVD_BOUNDS_OK(e - j <= TP && j % PG_TILES + e - j <= PG_TILES, P.status)) F.bytes = 0;  // (a part lies in one page, and in its stage)
+  }
+  F.bad = __ballot_sync(0xffffffffu, bad);
+}
+// the part that begins at or behind tile `at`, a multiple of TILES, if there is one
+template <int DH>
+__device__ __forceinline__ void c4_fetch(const C4Attend &P, const C4Span *spans, const C4Place &W, int lane, int at, uint32_t stage, C4Feed &F) {
+  if (at >= F.end) return;
+  int l = (at - F.base) / C4Cfg<DH>::TILES;
+  if (l >= 32) {
+    F.base = at;
+    c4_look_up<DH>(P, spans, W, lane, F);
+    l = 0;
+  }
+  F.unusable = (F.unusable & ~(1u << stage)) | (F.bad >> l & 1u) << stage;
+  if (lane == l) {
+    mbar_arrive_expect_tx(W.bars + 8 * stage, F.bytes);
+    if (F.bytes > 0) bulk_load(W.ring + stage * C4Cfg<DH>::STAGE, F.src, F.bytes, W.bars + 8 * stage, W.policy);
+  }
+}
+// A wait has run out.  The copies in flight land before the CTA's shared memory goes to another: each is waited for once more, whatever the abort flag
+// says.  The warp goes on through the merges, whose barriers count it.
+template <int DH>
+__device__ __forceinline__ void c4_give_up(const C4Attend &P, const C4Place &W, int lane, volatile int *abort_flag, const volatile int *never, C4Feed &F) {
+  constexpr int TP = C4Cfg<DH>::TILES, S = C4Cfg<DH>::STAGES;
+  raise(P.status, STATUS_TIMEOUT, abort_flag);
+  F.timed_out = true;
+  for (int j = F.i / TP * TP; j < min(F.end, F.i / TP * TP + S * TP); j += TP, ++F.attended)
+    warp_wait(W.bars + 8 * (F.attended % S), (F.attended / S) & 1, never, P.timeout_ns, lane);
+}
+// The rest of a run, from the first tile with a scale of 2 or more on; `ahead` tiles of its part have been attended
+template <int DH, int QB>
+__device__ __forceinline__ void c4_large(const C4Attend &P, const C4Span *spans, const C4Place &W, int lane, uint8_t *ring, const uint8_t *query, const uint32_t (&qf)[QB][4], float qs0,
+                                         float qs1, volatile int *abort_flag, const volatile int *never, int ahead, bool first, C4Feed &F, C4Sums<DH> &A) {
+  constexpr int TP = C4Cfg<DH>::TILES, S = C4Cfg<DH>::STAGES;
+  constexpr bool PLAIN = DH == 128;  // one tile at a time for both kinds, but for 128 channels: two plain ones at once 32.6 us, one 40.6
+  const int plain0 = spans[W.seq].plain0, plain1 = spans[W.seq].plain1;
+#pragma unroll 1
+  while (F.i < F.end) {
+    const uint32_t stage = F.attended % S;
+    if (!warp_wait(W.bars + 8 * stage, (F.attended / S) & 1, abort_flag, P.timeout_ns, lane)) {
+      c4_give_up<DH>(P, W, lane, abort_flag, never, F);
+      break;
+    }
+    const int next = min(F.end, F.i / TP * TP + TP);
+    uint8_t *at = ring + stage * C4Cfg<DH>::STAGE + ahead * PgTile<DH>::BYTES;
+    if (!(F.unusable >> stage & 1)) {
+      if (PLAIN && next - F.i == TP && F.i >= plain0 && next <= plain1) {
+        c4_attend<DH, TP, false, true>(at, query, qf, qs0, qs1, spans[W.seq], 0, first, lane, A);
+      } else {
+#pragma unroll 1
+        for (int x = F.i; x < next; ++x)
+          c4_attend<DH, 1, true, true>(at + (x - F.i) * PgTile<DH>::BYTES, query, qf, qs0, qs1, spans[W.seq], spans[W.seq].pos(x), first && x == F.i, lane, A,
+                                       x < plain0 || x >= plain1);
+      }
+      first = false;
+    }
+    ahead = 0;
+    F.i = next;
+    __syncwarp();
+    c4_fetch<DH>(P, spans, W, lane, next / TP * TP + (S - 1) * TP, stage, F);
+    ++F.attended;
+  }
+}
+// At 256 channels a function of its own, so that the code of the other runs lies together: inline, a call after other kernels' took 18.4 us instead of 16.4
+// (Gemma-3-4B layer, window of 1024), and a step of two sequences of the 34-layer stack 2.74 ms instead of 2.66; runs with such scales take 25.0 us
+// instead of 18.1 for it (32768 keys).  At 128 it would cost registers (31.7 us, 30.3).
+template <int DH, int QB>
+struct C4Large {
+  const C4Span *spans;
+  C4Place W;
+  C4Feed F;
+  C4Sums<DH> A;
+  uint32_t qf[QB][4];
+  float qs0, qs1;
+  uint8_t *ring;
+  const uint8_t *query;
+  volatile int *abort_flag;
+  const volatile int *never;
+  int ahead;
+  bool first;
+};
+template <int DH, int QB>
+__device__ __noinline__ void c4_large_apart(const C4Attend &P, C4Large<DH, QB> &L, int lane) {
+  C4Feed F = L.F;
+  C4Sums<DH> A = L.A;
+  const C4Place W = L.W;
+  c4_large<DH, QB>(P, L.spans, W, lane, L.ring, L.query, L.qf, L.qs0, L.qs1, L.abort_flag, L.never, L.ahead, L.first, F, A);
+  L.F = F;
+  L.A = A;
+}
+
 // The tiles of a sequence and KV head are cut into equal runs, one a CTA, of at least a tile for each warp and not more of them than the
 // launch has CTAs; where there are more sequences and heads than CTAs, a CTA has several whole ones.  Where either would leave a CTA with
 // far more tiles than the average, all tiles one after the other are cut into equal pieces instead, and a CTA has several runs, the first
@@ -688,7 +807,7 @@ __device__ __forceinline__ bool c4_attend(uint8_t *tile0, const uint8_t *query, 
 // their token's scale.  The weights are 2^(s - m'), m' = the reference maximum less 12 (c4_reference): fp16 rounds a weight like any other
 // down to 2^-26 of the largest one.  So that it does the same to the products with scales, these are taken 2^10 times as large where none of the head
 // is 2^-9 or more, and from the first one of 2 on each block's by a power of two that takes the largest below 2, in a loop of its own
-// (values of deviation 30: 32.8 us for 16 x 8192 keys of a Qwen3-4B layer, 30.5 otherwise; 18.1 and 15.4 for 32768 of a Gemma-3-4B one; with one power for the
+// (values of deviation 30: 35.1 us for 16 x 8192 keys of a Qwen3-4B layer, 30.3 otherwise; 25.0 and 15.2 for 32768 of a Gemma-3-4B one; with one power for the
 // whole head, which loses the small ones, 30.8 and 15.4).  One that this leaves below 2^-19 is left to a second turn over the tile.
 //
 // 16 x 8192 keys, 32 query on 8 KV heads of 128: 31.4 us for 146 MB (16-bit caches of the same keys take 106).  44 of 57 thousand clocks
@@ -810,63 +929,33 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
     seq = last_before(s_tiles, piece0);
   }
   uint32_t qf[QB][4];  // block b, step h: registers 2 h, 2 h + 1
-  bool timed_out = false;
-  uint32_t attended = 0;  // parts, over all runs
-  // ---- a run: tiles run0 .. run1 - 1 of the launch, of a sequence and head that begin at `begin`.  This warp's tiles of it and their copies:
-  // parts are what it has of TP aligned tiles.  Lane l knows the part that begins at or behind tile f_base + TP l.
-  int run0 = piece0, run1, head, begin, i, end, f_base, f_bytes = 0;
-  const uint8_t *f_src = nullptr;
-  uint32_t f_bad = 0, unusable = 0;  // parts without a page, stages that hold one
+  // ---- a run: tiles run0 .. run1 - 1 of the launch, of a sequence and head that begin at `begin`
+  int run0 = piece0, run1, begin;
+  C4Feed F;
+  C4Place W;
+  W.ring = smem_u32(ring);
+  W.bars = bars;
+  W.policy = read_once();  // (3 to 5 % of the call: 32768 keys of a Gemma-3-4B layer 16.8 -> 16.1 us, 30 x 2048 of a Qwen3-4B one 23.4 -> 22.4)
   constexpr int CH = DH / 32;        // channels of a query that a lane has; a warp takes a head
   uint32_t qw[CH / 2];
-  const uint64_t policy = read_once();  // (3 to 5 % of the call: 32768 keys of a Gemma-3-4B layer 16.8 -> 16.1 us, 30 x 2048 of a Qwen3-4B one 23.4 -> 22.4)
-  auto look_up = [&]() {
-    const C4Span &sp = s_span[seq];
-    const int j = max(i, f_base + TP * lane), e = min(end, f_base + TP * lane + TP);
-    bool bad = false;
-    f_bytes = 0;
-    if (j < e) {
-      const int pos = sp.pos(j);
-      const int page = P.table[static_cast<long long>(P.seq[seq]) * P.max_pages + pos / PG_TOKENS];
-      bad = page < 0 || page >= P.pages;
-      f_bytes = bad ? 0 : (e - j) * T::BYTES;
-      f_src = P.pool + (bad ? 0 : page) * P.page_bytes + (head * PG_TILES + j % PG_TILES) * T::BYTES;
-      if (bad) atomicOr(P.status, STATUS_POSITION);
-      if (!KVD_BOUNDS_OK(e - j <= TP && j % PG_TILES + e - j <= PG_TILES, P.status)) f_bytes = 0;  // (a part lies in one page, and in its stage)
-    }
-    f_bad = __ballot_sync(0xffffffffu, bad);
-  };
-  auto fetch = [&](int at, uint32_t stage) {  // the part that begins at or behind tile `at`, a multiple of TP, if there is one
-    if (at >= end) return;
-    int l = (at - f_base) / TP;
-    if (l >= 32) {
-      f_base = at;
-      look_up();
-      l = 0;
-    }
-    unusable = (unusable & ~(1u << stage)) | (f_bad >> l & 1u) << stage;
-    if (lane == l) {
-      mbar_arrive_expect_tx(bars + 8 * stage, f_bytes);
-      if (f_bytes > 0) bulk_load(smem_u32(ring) + stage * C::STAGE, f_src, f_bytes, bars + 8 * stage, policy);
-    }
-  };
   auto open_run = [&]() {  // the run that begins at run0: its queries and first parts are asked for
     while (s_tiles[seq + 1] <= run0) ++seq;
     const int tiles = s_span[seq].tiles;
-    head = (run0 - s_tiles[seq]) / tiles;
-    begin = s_tiles[seq] + head * tiles;
+    W.seq = seq;
+    W.head = (run0 - s_tiles[seq]) / tiles;
+    begin = s_tiles[seq] + W.head * tiles;
     run1 = min(piece1, begin + tiles);
     const bool some = warp < P.group;
-    const uint16_t *src = P.q + (static_cast<long long>(seq) * P.n_q + head * P.group + (some ? warp : 0)) * DH + lane * CH;
+    const uint16_t *src = P.q + (static_cast<long long>(seq) * P.n_q + W.head * P.group + (some ? warp : 0)) * DH + lane * CH;
 #pragma unroll
     for (int j = 0; j < CH / 2; ++j) qw[j] = some ? reinterpret_cast<const uint32_t *>(src)[j] : 0u;
-    i = run0 - begin + (run1 - run0) * warp / WARPS;
-    end = timed_out ? i : run0 - begin + (run1 - run0) * (warp + 1) / WARPS;
-    f_base = i / TP * TP;
-    if (i < end) {  // (every copy that is issued is waited for)
-      look_up();
+    F.i = run0 - begin + (run1 - run0) * warp / WARPS;
+    F.end = F.timed_out ? F.i : run0 - begin + (run1 - run0) * (warp + 1) / WARPS;
+    F.base = F.i / TP * TP;
+    if (F.i < F.end) {  // (every copy that is issued is waited for)
+      c4_look_up<DH>(P, s_span, W, lane, F);
 #pragma unroll
-      for (int j = 0; j < S; ++j) fetch(f_base + TP * j, (attended + j) % S);
+      for (int j = 0; j < S; ++j) c4_fetch<DH>(P, s_span, W, lane, F.base + TP * j, (F.attended + j) % S, F);
     }
   };
   open_run();
@@ -919,66 +1008,60 @@ __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_ca
 #pragma unroll
     for (uint32_t &limit : A.v_limit) limit = C4_TINY * 0x10001u;
     const int plain0 = s_span[seq].plain0, plain1 = s_span[seq].plain1;
-    // The parts of the run, up to one with a scale of 2 or more; with `Large` the tiles from there on.
-    bool first = true, large = false;
-    int ahead = 0;  // tiles of the part that have been attended
-    auto parts = [&](auto Large) {
-      constexpr bool LARGE = decltype(Large)::value, PLAIN = !LARGE || DH == 128;
+    // the parts of the run, up to one with a scale of 2 or more
+    bool first = true;
+    int ahead = 0;
+    auto usual_parts = [&]() {
 #pragma unroll 1
-      while (i < end) {
-        const uint32_t stage = attended % S;
-        if (!__all_sync(0xffffffffu, mbar_try_wait(bars + 8 * stage, (attended / S) & 1)) &&
-            !warp_wait(bars + 8 * stage, (attended / S) & 1, &s_abort, P.timeout_ns, lane)) {
-          raise(P.status, STATUS_TIMEOUT, &s_abort);
-          // The copies in flight land before the CTA's shared memory goes to another: each is waited for once more, whatever the abort flag
-          // says.  The warp goes on through the merges, whose barriers count it.
-          timed_out = true;
-          for (int j = i / TP * TP; j < min(end, i / TP * TP + S * TP); j += TP, ++attended)
-            warp_wait(bars + 8 * (attended % S), (attended / S) & 1, &s_never, P.timeout_ns, lane);
-          return;
+      while (F.i < F.end) {
+        const uint32_t stage = F.attended % S;
+        if (!__all_sync(0xffffffffu, mbar_try_wait(bars + 8 * stage, (F.attended / S) & 1)) &&
+            !warp_wait(bars + 8 * stage, (F.attended / S) & 1, &s_abort, P.timeout_ns, lane)) {
+          c4_give_up<DH>(P, W, lane, &s_abort, &s_never, F);
+          return true;
         }
-        const int next = min(end, i / TP * TP + TP);
+        const int next = min(F.end, F.i / TP * TP + TP);
         uint8_t *at = ring + stage * C::STAGE;
-        if (LARGE) {
-          at += ahead * T::BYTES;
-          ahead = 0;
-        }
-        if (!(unusable >> stage & 1)) {
-          if (PLAIN && next - i == TP && i >= plain0 && next <= plain1) {
-            if (!c4_attend<DH, TP, false, LARGE>(at, query, qf, qs0, qs1, s_span[seq], 0, first, lane, A)) {
-              large = true;
-              return;
-            }
+        if (!(F.unusable >> stage & 1)) {
+          if (next - F.i == TP && F.i >= plain0 && next <= plain1) {
+            if (!c4_attend<DH, TP, false, false>(at, query, qf, qs0, qs1, s_span[seq], 0, first, lane, A)) return false;
           } else {
 #pragma unroll 1
-            for (int x = i; x < next; ++x) {
-              // (with LARGE one tile at a time for both kinds, but for 128 channels: two plain ones at once 32.6 us, one 40.6)
-              if (!c4_attend<DH, 1, true, LARGE>(at + (x - i) * T::BYTES, query, qf, qs0, qs1, s_span[seq], s_span[seq].pos(x), first && x == i, lane, A,
-                                                  !LARGE || x < plain0 || x >= plain1)) {
-                large = true;
-                ahead = x - i;
-                i = x;
+            for (int x = F.i; x < next; ++x) {
+              if (!c4_attend<DH, 1, true, false>(at + (x - F.i) * T::BYTES, query, qf, qs0, qs1, s_span[seq], s_span[seq].pos(x), first && x == F.i, lane, A)) {
+                ahead = x - F.i;
+                F.i = x;
                 first = first && ahead == 0;
-                return;
+                return false;
               }
             }
           }
           first = false;
         }
-        i = next;
+        F.i = next;
         __syncwarp();
-        fetch(i / TP * TP + (S - 1) * TP, stage);
-        ++attended;
+        c4_fetch<DH>(P, s_span, W, lane, F.i / TP * TP + (S - 1) * TP, stage, F);
+        ++F.attended;
       }
+      return true;
     };
-    parts(std::false_type());
-    if (large) parts(std::true_type());
+    const bool large = !usual_parts();
+    if (large) {
+      if constexpr (DH < 256) {
+        c4_large<DH, QB>(P, s_span, W, lane, ring, query, qf, qs0, qs1, &s_abort, &s_never, ahead, first, F, A);
+      } else {
+        C4Large<DH, QB> L{s_span, W, F, A, {}, qs0, qs1, ring, query, &s_abort, &s_never, ahead, first};
+        c4_large_apart<DH, QB>(P, L, lane);
+        F = L.F;
+        A = L.A;
+      }
+    }
     // ---- the next run is asked for before the warps' sums of this one come together
     const bool whole = run1 - run0 == s_span[seq].tiles;
-    const long long out0 = static_cast<long long>(seq) * P.n_q + head * P.group;  // rows of the output
+    const long long out0 = static_cast<long long>(seq) * P.n_q + W.head * P.group;  // rows of the output
     const int slot = 2 * blockIdx.x + (run0 != piece0);
     if (!whole) {
-      if (tid == 0) s_parted[parted] = make_int2(seq, head);
+      if (tid == 0) s_parted[parted] = make_int2(seq, W.head);
       ++parted;
     }
     more = run1 < piece1;

@@ -2,20 +2,23 @@
 something else is broken; no run shows reliably what a late copy would write over.)"""
 import re
 
-from test_launch_rules import KERNELS
+from test_launch_rules import KERNELS, TEXT
 
 
 def test_copies_of_the_cache_are_waited_for_whatever_the_abort_flag_says():
-    body = KERNELS["kvd_cache4_attention_kernel"][1]
-    given_up = body[body.index("raise(P.status, STATUS_TIMEOUT"):]
-    given_up = given_up[:given_up.index("return;")]
-    waits = re.findall(r"warp_wait\(([^;]*)\);", given_up)
-    assert waits
-    for w in waits:  # not the flag that was just raised, but one that nobody raises; the limit stays
-        assert "&s_never" in w and "s_abort" not in w and "P.timeout_ns" in w
-    assert re.findall(r"s_never\s*=[^;]*;", body) == ["s_never = 0;"] and body.count("s_never") == 2 + len(waits)
+    text, body = TEXT["kvd_cache4.cu"], KERNELS["kvd_cache4_attention_kernel"][1]
+    given_up = text[text.index("void c4_give_up("):text.index("c4_large(")]
+    behind = given_up[given_up.index("raise(P.status, STATUS_TIMEOUT, abort_flag);"):]
+    # not the flag that was just raised, but one that nobody raises; the limit stays
+    assert re.findall(r"warp_wait\(([^;]*)\);", behind) == ["W.bars + 8 * (F.attended % S), (F.attended / S) & 1, never, P.timeout_ns, lane"]
+    assert re.findall(r"s_never\s*=[^;]*;", body) == ["s_never = 0;"] and not re.search(r"\*never\s*=", text)
     # all parts that may be on their way: as many as the ring has stages
-    assert re.search(r"for \(int j = i / TP \* TP; j < min\(end, i / TP \* TP \+ S \* TP\); j \+= TP, \+\+attended\)", given_up)
+    assert "for (int j = F.i / TP * TP; j < min(F.end, F.i / TP * TP + S * TP); j += TP, ++F.attended)" in given_up
+    # every wait for a copy that runs out goes there, with both flags
+    waits = [m.end() for m in re.finditer(r"!warp_wait\([^;{]*\{", text)]
+    assert len(waits) == 2 and all(text[at:].lstrip().startswith("c4_give_up<DH>(") for at in waits)
+    assert text.count("STATUS_TIMEOUT") == 1
+    assert "&s_abort, &s_never, F)" in body and re.search(r"c4_large<DH, QB>\([^;]*&s_abort, &s_never", body) and re.search(r"C4Large<DH, QB> L\{[^;]*&s_abort, &s_never", body)
 
 
 def test_a_cta_of_a_cluster_keeps_its_memory_for_the_others():
