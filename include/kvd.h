@@ -529,8 +529,9 @@ kvd_status kvd_pages_compact(kvd_ctx *ctx, const kvd_paged_cache *in, const kvd_
  * counts[0] tokens of seqs[0], then counts[1] of seqs[1] and so on (HOST, n <= KVD_MAX_PAGE_SEQS, sequences all different); token j of
  * entry i goes to position first[i] + j (DEVICE int32 [n]) of its sequence in `layer`.  first[i] < 0: the entry is left out.  A
  * position beyond the sequence's lens, or a page number outside the pool, is left out and recorded (KVD_ERR_POSITION).  Positions
- * from first_out on are the sequence's own; writing an earlier one again changes every sequence that shares its page.  Keys come as
- * attention reads them, rotated.  One launch. */
+ * from first_out on are the sequence's own; writing an earlier one again changes every sequence that shares its page, and two entries of
+ * a call must not do that to the same pair of positions 2 p, 2 p + 1 of a shared page.  Keys come as attention reads them, rotated.
+ * One launch. */
 kvd_status kvd_cache4_append(kvd_ctx *ctx, const kvd_paged_cache *cache, int layer, int n, const int32_t *seqs,
                              const int32_t *counts, const int32_t *first, const void *k, const void *v, int64_t row_stride,
                              void *stream);

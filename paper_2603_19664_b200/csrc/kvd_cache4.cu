@@ -136,7 +136,8 @@ __device__ __forceinline__ uint8_t *c4_page(const C4Rows<N> &P, C4Job &J) {
 // Four lanes take a block of both tokens of a pair, 16 bytes of each row apiece; its scale is the maximum over the four.  A thread takes
 // up to four such pieces, whose rows it asks for before it knows the page.  2 bytes per value are read, 4.5 bits written: 16004 tokens
 // of a Qwen3-4B layer 20 us, 84 MB (4.2 TB/s), issue slots at 72 % (14 instructions a value, 3.5 of them the quotient), and 15 to
-// read them back (5.6 TB/s).  Rows, in both directions, are the first to leave the second-level cache (39.2 -> 36.9 us for both).
+// read them back (5.6 TB/s).  Rows, in both directions, are the first to leave the second-level cache (39.2 -> 36.9 us for both;
+// attention of 256 rows over 4096 that were read back takes 38.9 us with the call either way).
 // Packed fp32 arithmetic for the quotients: 3 % slower here, 4 % faster at 256 channels.
 template <int DH, int F16, int N>
 __global__ void __launch_bounds__(C4_ROW_THREADS) kvd_cache4_append_kernel(const __grid_constant__ C4Rows<N> P) {
@@ -376,7 +377,8 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// What a launch reads once is the first to leave the second-level cache.
+// Tiles are the first to leave the second-level cache.  (Most are read once.  Pages that sequences share are read by each of them, and no slower for it: 16
+// continuations of one prompt of 8192 keys, Qwen3-4B layer, 31.2 us with and without, 37.5 and 37.2 behind other data.)
 __device__ __forceinline__ uint64_t read_once() {
   uint64_t policy;
   asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
@@ -810,11 +812,11 @@ __device__ __noinline__ void c4_large_apart(const C4Attend &P, C4Large<DH, QB> &
 // (values of deviation 30: 35.1 us for 16 x 8192 keys of a Qwen3-4B layer, 30.3 otherwise; 25.0 and 15.2 for 32768 of a Gemma-3-4B one; with one power for the
 // whole head, which loses the small ones, 30.8 and 15.4).  One that this leaves below 2^-19 is left to a second turn over the tile.
 //
-// 16 x 8192 keys, 32 query on 8 KV heads of 128: 31.4 us for 146 MB (16-bit caches of the same keys take 106).  44 of 57 thousand clocks
+// 16 x 8192 keys, 32 query on 8 KV heads of 128: 31.8 us for 146 MB (16-bit caches of the same keys take 106).  44 of 57 thousand clocks
 // are the tiles, at 6.3 TB/s: bound by memory then, at 2 to 3 instructions a clock and SM (2 products, 8 conversions and some 6
 // of scales for a block of 32 channels and 16 keys; with spilled registers, or with 16 warps of 128, the instructions were what bound it,
 // 10 % longer).  6 are the start (lengths, page numbers, queries, the first copies: four latencies one after the other), 4 the merge
-// of the warps.  One sequence of 32768 keys, 8 on 4 of 256: 16.1 us for 38 MB: start 5, tiles 12 (5.9 TB/s), merge of the warps 2,
+// of the warps.  One sequence of 32768 keys, 8 on 4 of 256: 16.2 us for 38 MB: start 5, tiles 12 (5.9 TB/s), merge of the warps 2,
 // count 2, last merge 4.
 template <int DH, int F16>
 __global__ void __launch_bounds__(C4Cfg<DH>::WARPS * 32, C4Cfg<DH>::CTAS) kvd_cache4_attention_kernel(const __grid_constant__ C4Attend P) {

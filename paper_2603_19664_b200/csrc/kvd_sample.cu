@@ -6,10 +6,10 @@
 // dealt out evenly, and running sums over them, from the largest, give the threshold; a value's mass is its count times one
 // exponential.  A second walk over the row, in order of columns, adds the masses of what stays, looked up by value, and finds the column.
 //
-// 64 rows of 151936 bf16 logits, two CTAs a row: 40 us in a graph (19 MB, 3 us at the copy rate).  The counts take 17 of the 75 thousand clocks (a
+// 64 rows of 151936 bf16 logits, two CTAs a row: 41 us in a graph (19 MB, 3 us at the copy rate; fp16 52).  The counts take 17 of the 75 thousand clocks (a
 // shared-memory atomic of random addresses 7 a warp: the banks' conflicts, twice), the second walk 20 where all columns stay
 // (one look-up a column: 3.5 a warp, and as many issue slots), and some fifteen steps that end in a barrier over the CTA or the
-// cluster 1 to 3 each: rows of 1000 take 17.7 us, and a single one of 49152 on eight CTAs 20.
+// cluster 1 to 3 each: rows of 1000 take 18 us, and a single one of 49152 on eight CTAs 17 to 21.
 //
 // Masses are whole numbers, in units of 2^-44 of the largest logit's: sums of them are exact in any order, so that the token does not
 // depend on how a row is cut, and a border between two tokens is off by 1e-11 of the mass (a token in a flat tail weighs
